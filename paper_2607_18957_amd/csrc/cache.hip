@@ -1,0 +1,231 @@
+// ii_cache_write and ii_cache_read: a paged key/value cache, quantised as it
+// is written.
+//
+// A block of 32 elements x gets the scale 2^e, e the least with max |x| <=
+// 448 * 2^e over its finite elements, and codes e4m3(x * 2^-e). Both the
+// scale and the product are exact, so the codes are the definition's, bit for
+// bit, at any precision.
+//
+// Bound by memory: each lane moves 16 bytes of activations (8 elements) of
+// keys or of values, four lanes hold a block and agree on its scale by two
+// exchanges, so reads and writes of a head's row are contiguous.
+#include "ops.h"
+#include "ops_device.h"
+
+namespace ii {
+namespace {
+
+struct Cache {
+    uint8_t* at[2];  // keys, values; bytes
+    uint8_t* scale[2];
+    int64_t page_stride, head_stride, token_stride;  // bytes
+    int64_t scale_page_stride, scale_head_stride, scale_token_stride;
+    int64_t pages;
+    int32_t page_bits;
+};
+
+struct Tokens {
+    uint8_t* at[2];
+    int64_t token_stride[2], head_stride[2];  // bytes
+    const int64_t* slots;
+    int64_t tokens;
+    int32_t heads, dim;
+};
+
+constexpr int kThreads = 256;
+
+// Exponent (biased) of a block's scale from the bits of its largest finite
+// magnitude: amax = 1.f * 2^E fits 448 = 1.75 * 2^8 at 2^(E - 8), or needs
+// one more if f > 0.75.
+__device__ inline uint32_t scale_exponent(uint32_t amax) {
+    const int e = (int)(amax >> 23) - 8 + ((amax & 0x7fffff) > 0x600000);
+    return e < 1 ? 1 : e;  // at most 247
+}
+
+template <class T, bool kQuant, bool kWrite>
+__global__ __launch_bounds__(kThreads) void cache_move(Cache c, Tokens f) {
+    using x8 = typename Vec<T>::x8;
+    const int per_head = f.dim / 8;
+    const int64_t per_token = (int64_t)per_head * f.heads;
+    const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int kv = blockIdx.y;
+    const int64_t token = unit / per_token;
+    const bool live = token < f.tokens;
+    const int in = (int)(unit - token * per_token), head = in / per_head, part = in % per_head;
+    // every lane takes part in the exchanges below; blocks are four
+    // neighbouring lanes of one token
+    const int64_t slot = live ? f.slots[token] : -1;
+    const int64_t page = slot >> c.page_bits;
+    const bool kept = slot >= 0 && page < c.pages;
+    const int64_t row = slot & (((int64_t)1 << c.page_bits) - 1);
+    const int64_t at = page * c.page_stride + head * c.head_stride + row * c.token_stride;
+    const int64_t sat = page * c.scale_page_stride + head * c.scale_head_stride +
+                        row * c.scale_token_stride + part / 4;
+    x8* user = reinterpret_cast<x8*>(f.at[kv] + token * f.token_stride[kv] +
+                                     head * f.head_stride[kv] + part * 16);
+    if (!kQuant) {
+        u32x4* mine = reinterpret_cast<u32x4*>(c.at[kv] + at + part * 16);
+        u32x4* theirs = reinterpret_cast<u32x4*>(user);
+        if (kWrite) {
+            if (kept) *mine = *theirs;
+        } else if (live) {
+            *theirs = kept ? *mine : u32x4{};
+        }
+        return;
+    }
+    if (kWrite) {
+        x8 v = {};
+        if (kept) v = *user;
+        uint32_t amax = 0;
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = (float)v[j];
+            const uint32_t b = __builtin_bit_cast(uint32_t, x[j]) & 0x7fffffff;
+            if (b < 0x7f800000 && b > amax) amax = b;
+        }
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+        const uint32_t e = scale_exponent(amax);
+        const float inverse = __builtin_bit_cast(float, (254 - e) << 23);
+        // 2^8 times a code above 240 is past the largest f16
+        const float most = sizeof(T) == 2 && __is_same(T, _Float16) && e == 127 + 8 ? 240.0f : 448.0f;
+        uint32_t code[2] = {};
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            float y[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t b = __builtin_bit_cast(uint32_t, x[j + i]) & 0x7fffffff;
+                y[i] = b < 0x7f800000 ? fminf(fmaxf(x[j + i] * inverse, -most), most)
+                                      : __builtin_nanf("");
+            }
+            int& w = reinterpret_cast<int&>(code[j / 4]);
+            w = j % 4 ? __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], w, true)
+                      : __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], w, false);
+        }
+        if (kept) {
+            *reinterpret_cast<u32x2*>(c.at[kv] + at + part * 8) = u32x2{code[0], code[1]};
+            if (part % 4 == 0) c.scale[kv][sat] = (uint8_t)e;
+        }
+    } else if (live) {
+        x8 v = {};
+        if (kept) {
+            const u32x2 code = *reinterpret_cast<const u32x2*>(c.at[kv] + at + part * 8);
+            // 2^(e - 127); an exponent of 0 (2^-127) is below float's normal range
+            const uint32_t e = c.scale[kv][sat];
+            const float scale = __builtin_bit_cast(float, e ? e << 23 : 0x400000u);
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(code[j / 4], false);
+                const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(code[j / 4], true);
+                v[j] = (T)(lo[0] * scale);
+                v[j + 1] = (T)(lo[1] * scale);
+                v[j + 2] = (T)(hi[0] * scale);
+                v[j + 3] = (T)(hi[1] * scale);
+            }
+        }
+        *user = v;
+    }
+}
+
+template <class T>
+void launch(const Cache& c, const Tokens& f, bool quant, bool write, hipStream_t stream) {
+    // a dispatch counts its work-items in 32 bits
+    const int64_t per_token = (int64_t)f.heads * (f.dim / 8);
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 31) / per_token);
+    for (int64_t t0 = 0; t0 < f.tokens; t0 += most) {
+        Tokens part = f;
+        part.tokens = std::min(most, f.tokens - t0);
+        part.slots += t0;
+        for (int i = 0; i < 2; ++i) part.at[i] += t0 * f.token_stride[i];
+        const dim3 grid((uint32_t)((part.tokens * per_token + kThreads - 1) / kThreads), 2);
+        if (quant && write)
+            cache_move<T, true, true><<<grid, kThreads, 0, stream>>>(c, part);
+        else if (quant)
+            cache_move<T, true, false><<<grid, kThreads, 0, stream>>>(c, part);
+        else if (write)
+            cache_move<T, false, true><<<grid, kThreads, 0, stream>>>(c, part);
+        else
+            cache_move<T, false, false><<<grid, kThreads, 0, stream>>>(c, part);
+    }
+}
+
+int move(const char* fn, const ii_cache* ca, const ii_tokens* tk, bool write, hipStream_t stream) {
+    if (!ca || !tk) return fail(II_EINVAL, "%s: an argument is NULL", fn);
+    const ii_cache& c = *ca;
+    const ii_tokens& f = *tk;
+    CacheRows held;
+    int rc = check_cache(fn, c, &held);
+    if (rc) return rc;
+    if (!half_type(f.dtype)) return fail(II_EINVAL, "%s: dtype %d", fn, f.dtype);
+    if (c.dtype != II_FP8_E4M3 && c.dtype != f.dtype)
+        return fail(II_EINVAL, "%s: a cache of type %d, tokens of type %d", fn, c.dtype, f.dtype);
+    if (f.reserved) return fail(II_EINVAL, "%s: reserved is %d", fn, f.reserved);
+    if (f.tokens < 0 || f.tokens > (int64_t)1 << 40)
+        return fail(II_EINVAL, "%s: %lld tokens", fn, (long long)f.tokens);
+    if (!f.tokens) return II_OK;
+    Rows slots, rows[2];
+    rc = check_rows(fn, "slots", f.slots, 1, (uint64_t)f.tokens * 8, 0, 8, &slots);
+    if (rc) return rc;
+    const int64_t ts[2] = {f.k_token_stride, f.v_token_stride};
+    const int64_t hs[2] = {f.k_head_stride, f.v_head_stride};
+    void* const at[2] = {f.k, f.v};
+    const char* const what[2] = {"k", "v"};
+    for (int i = 0; i < 2; ++i) {
+        rc = check_heads(fn, what[i], at[i], f.tokens, c.heads, c.dim, ts[i], hs[i], 2, !write,
+                         &rows[i]);
+        if (rc) return rc;
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (!write && (rc = check_apart(fn, "slots", rows[i], slots))) return rc;
+        for (const Rows& r : held.all) {
+            rc = write ? check_apart(fn, what[i], r, rows[i]) : check_apart(fn, "the cache", rows[i], r);
+            if (rc) return rc;
+        }
+    }
+    if (write)
+        for (const Rows& r : held.all)
+            if ((rc = check_apart(fn, "slots", r, slots))) return rc;
+    if (!write && (rc = check_apart(fn, "v", rows[0], rows[1]))) return rc;
+    Cache d;
+    const int size = c.dtype == II_FP8_E4M3 ? 1 : 2;
+    d.at[0] = static_cast<uint8_t*>(c.k);
+    d.at[1] = static_cast<uint8_t*>(c.v);
+    d.scale[0] = c.k_scale;
+    d.scale[1] = c.v_scale;
+    d.page_stride = c.page_stride * size;
+    d.head_stride = c.head_stride * size;
+    d.token_stride = c.token_stride * size;
+    d.scale_page_stride = c.scale_page_stride;
+    d.scale_head_stride = c.scale_head_stride;
+    d.scale_token_stride = c.scale_token_stride;
+    d.pages = c.pages;
+    d.page_bits = __builtin_ctz(c.page);
+    Tokens t;
+    for (int i = 0; i < 2; ++i) {
+        t.at[i] = static_cast<uint8_t*>(at[i]);
+        t.token_stride[i] = ts[i] * 2;
+        t.head_stride[i] = hs[i] * 2;
+    }
+    t.slots = f.slots;
+    t.tokens = f.tokens;
+    t.heads = c.heads;
+    t.dim = c.dim;
+    if (f.dtype == II_BF16)
+        launch<__bf16>(d, t, size == 1, write, stream);
+    else
+        launch<_Float16>(d, t, size == 1, write, stream);
+    return launched(fn);
+}
+
+}  // namespace
+}  // namespace ii
+
+extern "C" int ii_cache_write(const ii_cache* cache, const ii_tokens* from, hipStream_t stream) {
+    return ii::move("ii_cache_write", cache, from, true, stream);
+}
+
+extern "C" int ii_cache_read(const ii_cache* cache, const ii_tokens* to, hipStream_t stream) {
+    return ii::move("ii_cache_read", cache, to, false, stream);
+}

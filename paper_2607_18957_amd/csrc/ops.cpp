@@ -1,0 +1,142 @@
+// Argument checks of the operators.
+#include "ops.h"
+
+namespace ii {
+
+int check_rows(const char* fn, const char* what, const void* p, uint64_t rows, uint64_t width,
+               uint64_t stride, uint64_t align, Rows* r) {
+    *r = Rows{reinterpret_cast<uint64_t>(p), rows, width, stride};
+    if (!rows || !width) return II_OK;
+    if (!p) return fail(II_EINVAL, "%s: %s is NULL", fn, what);
+    if (r->at % align || (rows > 1 && stride % align))
+        return fail(II_EALIGN, "%s: %s (%#llx, stride %llu bytes) is not a multiple of %llu bytes",
+                    fn, what, (unsigned long long)r->at, (unsigned long long)stride,
+                    (unsigned long long)align);
+    uint64_t span, end;
+    if (__builtin_mul_overflow(rows - 1, stride, &span) ||
+        __builtin_add_overflow(span, width, &span) || __builtin_add_overflow(r->at, span, &end))
+        return fail(II_EOVERFLOW, "%s: %s: %llu rows of %llu bytes at stride %llu", fn, what,
+                    (unsigned long long)rows, (unsigned long long)width,
+                    (unsigned long long)stride);
+    if (!reachable(alloc_info(r->at), r->at, end))
+        return fail(II_EINVAL, "%s: %s [%#llx, +%llu bytes) is not memory the device can reach: "
+                    "not inside one device allocation or one pinned host allocation", fn, what,
+                    (unsigned long long)r->at, (unsigned long long)span);
+    return II_OK;
+}
+
+int check_apart(const char* fn, const char* what, const Rows& w, const Rows& r) {
+    if (!w.rows || !w.width || !r.rows || !r.width) return II_OK;
+    if (w.end() <= r.at || r.end() <= w.at) return II_OK;
+    if (w.rows > 1 && r.rows > 1 && w.stride == r.stride && w.width <= w.stride) {
+        const uint64_t s = w.stride;
+        const uint64_t d = w.at >= r.at ? (w.at - r.at) % s : (s - (r.at - w.at) % s) % s;
+        if (d >= r.width && d + w.width <= s) return II_OK;
+    }
+    return fail(II_EOVERLAP, "%s: what is written overlaps %s", fn, what);
+}
+
+int check_span(const char* fn, const char* what, const Axis* axes, int n, uint64_t width,
+               bool apart, uint64_t* span) {
+    Axis by[4];
+    int live = 0;
+    for (int i = 0; i < n; ++i) {
+        if (axes[i].count <= 1) continue;
+        if (axes[i].stride < 0) return fail(II_EINVAL, "%s: a stride of %s is negative", fn, what);
+        int j = live++;
+        for (; j > 0 && by[j - 1].stride > axes[i].stride; --j) by[j] = by[j - 1];
+        by[j] = axes[i];
+    }
+    uint64_t end = width;
+    for (int i = 0; i < live; ++i) {
+        if (apart && (uint64_t)by[i].stride < end)
+            return fail(II_EINVAL, "%s: rows of %s meet (stride %lld bytes, %llu held)", fn, what,
+                        (long long)by[i].stride, (unsigned long long)end);
+        uint64_t more;
+        if (__builtin_mul_overflow((uint64_t)by[i].count - 1, (uint64_t)by[i].stride, &more) ||
+            __builtin_add_overflow(end, more, &end) || end > INT64_MAX)
+            return fail(II_EOVERFLOW, "%s: the extent of %s", fn, what);
+    }
+    *span = end;
+    return II_OK;
+}
+
+int check_heads(const char* fn, const char* what, const void* p, int64_t tokens, int64_t heads,
+                int64_t dim, int64_t token_stride, int64_t head_stride, int size, bool written,
+                Rows* r) {
+    if (!tokens) {
+        *r = Rows{};
+        return II_OK;
+    }
+    int64_t ts, hs;
+    if (__builtin_mul_overflow(token_stride, (int64_t)size, &ts) ||
+        __builtin_mul_overflow(head_stride, (int64_t)size, &hs))
+        return fail(II_EOVERFLOW, "%s: the strides of %s", fn, what);
+    if ((tokens > 1 && ts % 16) || (heads > 1 && hs % 16))
+        return fail(II_EALIGN, "%s: strides of %s (%lld, %lld bytes) are not multiples of 16 bytes",
+                    fn, what, (long long)ts, (long long)hs);
+    const Axis axes[2] = {{tokens, ts}, {heads, hs}};
+    uint64_t token, span;
+    int rc = check_span(fn, what, axes + 1, 1, dim * size, written, &token);
+    if (!rc) rc = check_span(fn, what, axes, 2, dim * size, written, &span);
+    if (rc) return rc;
+    // tokens one after another, or one range
+    if (tokens > 1 && token <= (uint64_t)ts) return check_rows(fn, what, p, tokens, token, ts, 16, r);
+    return check_rows(fn, what, p, 1, span, 0, 16, r);
+}
+
+int check_cache(const char* fn, const ii_cache& c, CacheRows* held) {
+    const bool quant = c.dtype == II_FP8_E4M3;
+    if (!quant && !half_type(c.dtype)) return fail(II_EINVAL, "%s: cache of type %d", fn, c.dtype);
+    if (c.heads < 1) return fail(II_EINVAL, "%s: cache of %d heads", fn, c.heads);
+    if (c.dim != 64 && c.dim != 128) return fail(II_EINVAL, "%s: heads of %d elements", fn, c.dim);
+    if (c.page < 1 || (c.page & (c.page - 1)))
+        return fail(II_EINVAL, "%s: pages of %d tokens, not a power of two", fn, c.page);
+    if (c.pages < 0 || c.pages > INT32_MAX)
+        return fail(II_EINVAL, "%s: %lld pages", fn, (long long)c.pages);
+    *held = CacheRows{};
+    if (!c.pages) return II_OK;
+    const int64_t size = quant ? 1 : 2;
+    const char* const what[4] = {"the cache's k", "the cache's v", "k_scale", "v_scale"};
+    const void* const at[4] = {c.k, c.v, c.k_scale, c.v_scale};
+    const int arrays = quant ? 4 : 2;
+    uint64_t span[4];
+    for (int i = 0; i < arrays; ++i) {
+        Axis axes[3] = {{c.pages, c.page_stride}, {c.heads, c.head_stride}, {c.page, c.token_stride}};
+        if (i >= 2) {
+            axes[0].stride = c.scale_page_stride;
+            axes[1].stride = c.scale_head_stride;
+            axes[2].stride = c.scale_token_stride;
+        }
+        const int64_t align = i < 2 ? 16 : c.dim / 32;
+        for (Axis& a : axes) {
+            if (__builtin_mul_overflow(a.stride, i < 2 ? size : 1, &a.stride))
+                return fail(II_EOVERFLOW, "%s: the strides of %s", fn, what[i]);
+            if (a.count > 1 && a.stride % align)
+                return fail(II_EALIGN, "%s: a stride of %s (%lld bytes) is not a multiple of %lld "
+                            "bytes", fn, what[i], (long long)a.stride, (long long)align);
+        }
+        const int rc = check_span(fn, what[i], axes, 3, i < 2 ? c.dim * size : c.dim / 32, true,
+                                  &span[i]);
+        if (rc) return rc;
+    }
+    for (int i = 0; i < arrays; ++i) {
+        const int rc = check_rows(fn, what[i], at[i], 1, span[i], 0, i < 2 ? 16 : c.dim / 32,
+                                  &held->all[i]);
+        if (rc) return rc;
+    }
+    return II_OK;
+}
+
+int check_work(const char* fn, const void* work, uint64_t bytes) {
+    if (!work && !bytes) return II_OK;
+    Rows r;
+    return check_rows(fn, "work", work, 1, bytes, 0, 16, &r);
+}
+
+int launched(const char* fn) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? II_OK : fail(II_EHIP, "%s: %s", fn, hipGetErrorString(e));
+}
+
+}  // namespace ii

@@ -1,0 +1,56 @@
+// Element types and matrix instructions of the operators' kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace ii {
+
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+using f32x16 = __attribute__((ext_vector_type(16))) float;
+using u32x2 = __attribute__((ext_vector_type(2))) uint32_t;
+using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
+using bf16x4 = __attribute__((ext_vector_type(4))) __bf16;
+using f16x4 = __attribute__((ext_vector_type(4))) _Float16;
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using s16x4 = __attribute__((ext_vector_type(4))) short;
+
+template <class T>
+struct Vec;
+template <>
+struct Vec<__bf16> {
+    using x2 = bf16x2;
+    using x4 = bf16x4;
+    using x8 = bf16x8;
+};
+template <>
+struct Vec<_Float16> {
+    using x2 = f16x2;
+    using x4 = f16x4;
+    using x8 = f16x8;
+};
+
+// 16 rows of a times 16 rows of b over 32 elements: lane l holds elements
+// 8 (l / 16) .. + 8 of row l mod 16 of each, and of the sum rows
+// 4 (l / 16) + r of a against row l mod 16 of b.
+__device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+// 32 rows of a times 32 rows of b over 16 elements: lane l holds elements
+// 8 (l / 32) .. + 8 of row l mod 32, and of the sum rows
+// 8 (r / 4) + 4 (l / 32) + r mod 4 of a against row l mod 32 of b.
+__device__ inline f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+}  // namespace ii

@@ -19,6 +19,9 @@ struct AllocInfo {
     uint64_t device_at = 0;  // pinned host memory: the address kernels see it at
 };
 
+// What HIP reports about the allocation holding address x (runtime.hip).
+AllocInfo alloc_info(uint64_t x);
+
 // Whether copies may touch [b, e), given what is reported for address b: the
 // whole range must lie inside that one allocation. Pageable host memory and
 // unknown addresses are never reachable; a pinned host range whose allocation

@@ -500,7 +500,7 @@ static int ensure_trace(Runtime* r, size_t K) {
 // argument checks
 
 // What HIP reports about the allocation holding address x.
-static AllocInfo alloc_info(uint64_t x) {
+AllocInfo alloc_info(uint64_t x) {
     AllocInfo info;
     hipPointerAttribute_t a;
     if (hipPointerGetAttributes(&a, reinterpret_cast<void*>(x)) != hipSuccess) {
