@@ -53,4 +53,32 @@ __device__ inline f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+// Workgroups that share a result leave their parts in global memory; the last
+// to arrive joins them, in the order of their places. The workgroups run on
+// XCDs whose L2 caches do not see each other, so parts are written and read by
+// accesses of agent scope, which go past those caches. Nothing else passes
+// between the workgroups, so it is enough that a wave's writes have arrived
+// before it counts itself: a fence of agent scope would also write back the
+// whole L2, which took 130 us where 512 workgroups of a 20 us kernel did it.
+__device__ inline void leave_part(float* at, float v) {
+    __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline float take_part(const float* at) {
+    return __hip_atomic_load(const_cast<float*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// Whether this workgroup is the last of `parts`; the counter is zero again
+// then. Called by every thread, after the parts were left.
+__device__ inline bool arrive_last(uint32_t* counter, uint32_t parts) {
+    __shared__ uint32_t before;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == parts - 1)
+            __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return before == parts - 1;
+}
+
 }  // namespace ii
