@@ -348,6 +348,137 @@ __global__ __launch_bounds__(kRowWaves * kKGroups * 64) void linear_shared(Linea
     }
 }
 
+// Many tokens: 256 tokens by 256 weight rows (with a gate 128 of w and 128 of
+// w2, in turn by 16) a workgroup of eight waves, each 128 tokens by 64 rows.
+// Both operands go from memory straight into LDS, 64 elements of k at a time,
+// the next ones while these are multiplied. An LDS row is 128 bytes, its
+// 16-byte words exchanged by the row's last three bits, so that the eight
+// lanes of one LDS cycle, a row each, meet all banks.
+constexpr int kTile = 256, kTileK = 64, kTileWaves = 8;
+
+using Rsrc = __amdgpu_buffer_rsrc_t;
+
+__device__ inline Rsrc rows_rsrc(const void* base, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0,
+                                             (int)(uint32_t)min(bytes, (int64_t)0xffffffffll),
+                                             0x00020000);
+}
+
+template <class T, bool kGated>
+__global__ __launch_bounds__(kTileWaves * 64) void linear_tile(Linear<T> p, int tiles_m,
+                                                               int tiles_n) {
+    using x8 = typename Vec<T>::x8;
+    __shared__ __attribute__((aligned(1024))) T ws0[kTile * kTileK];
+    __shared__ __attribute__((aligned(1024))) T ws1[kTile * kTileK];
+    __shared__ __attribute__((aligned(1024))) T xs0[kTile * kTileK];
+    __shared__ __attribute__((aligned(1024))) T xs1[kTile * kTileK];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int row = lane % 16, part = lane / 16;
+
+    // workgroups go to the 8 XCDs in turn: each XCD gets a run of tiles, in
+    // bands of 4 tiles of tokens, so that the tiles its L2 serves at one time
+    // share rows
+    const int total = tiles_m * tiles_n, xcd = blockIdx.x % 8, place = blockIdx.x / 8;
+    const int tile = xcd * (total / 8) + min(xcd, total % 8) + place;
+    constexpr int kBand = 4;
+    const int band = tile / (kBand * tiles_n), in_band = tile % (kBand * tiles_n);
+    const int high = min(kBand, tiles_m - band * kBand);
+    const int tm = band * kBand + in_band % high, tn = in_band / high;
+
+    constexpr int kCols = kGated ? kTile / 2 : kTile;  // columns of out
+    const int64_t m0 = (int64_t)tm * kTile, n0 = (int64_t)tn * kCols;
+
+    // what this wave brings: 32 rows of each operand, 8 rows an instruction
+    const int64_t n_end = p.n - 1 - n0, m_end = p.m - 1 - m0;
+    const Rsrc wr = rows_rsrc(p.w + n0 * p.w_stride, (n_end * p.w_stride + p.k) * 2);
+    const Rsrc w2r = kGated ? rows_rsrc(p.w2 + n0 * p.w2_stride, (n_end * p.w2_stride + p.k) * 2) : wr;
+    const Rsrc xr = rows_rsrc(p.x + m0 * p.x_stride, (m_end * p.x_stride + p.k) * 2);
+    int woff[4], xoff[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = wave * 32 + i * 8 + lane / 8, word = (lane % 8) ^ (r % 8);
+        const int64_t c = kGated ? r / 32 * 16 + r % 16 : r;
+        const int64_t stride = kGated && i >= 2 ? p.w2_stride : p.w_stride;
+        woff[i] = (int)((min(c, n_end) * stride + word * 8) * 2);
+        xoff[i] = (int)((min((int64_t)r, m_end) * p.x_stride + word * 8) * 2);
+    }
+    auto bring = [&](int k, T* ws, T* xs) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                kGated && i >= 2 ? w2r : wr,
+                (__attribute__((address_space(3))) void*)(ws + (wave * 32 + i * 8) * kTileK), 16,
+                woff[i], k * 2, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                xr, (__attribute__((address_space(3))) void*)(xs + (wave * 32 + i * 8) * kTileK), 16,
+                xoff[i], k * 2, 0, 0);
+        }
+    };
+    const int wn = wave % 4 * 64, wm = wave / 4 * 128;
+    f32x4 acc[4][8] = {};
+    auto multiply = [&](const T* ws, const T* xs) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            x8 a[4], b[8];
+            const int word = ((s * 4 + part) ^ (row % 8)) * 8;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                a[i] = *reinterpret_cast<const x8*>(ws + (wn + i * 16 + row) * kTileK + word);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                b[j] = *reinterpret_cast<const x8*>(xs + (wm + j * 16 + row) * kTileK + word);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][j] = mfma16(a[i], b[j], acc[i][j]);
+        }
+    };
+    const int steps = p.k / kTileK;
+    if (steps > 0) bring(0, ws0, xs0);
+    for (int t = 0; t < steps; t += 2) {
+        __syncthreads();
+        if (t + 1 < steps) bring((t + 1) * kTileK, ws1, xs1);
+        multiply(ws0, xs0);
+        if (t + 1 < steps) {
+            __syncthreads();
+            if (t + 2 < steps) bring((t + 2) * kTileK, ws0, xs0);
+            multiply(ws1, xs1);
+        }
+    }
+    if (p.k % kTileK) {  // the rest of k: words past it are zero
+        __syncthreads();
+        const int k0 = steps * kTileK;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = wave * 32 + i * 8 + lane / 8, word = (lane % 8) ^ (r % 8);
+            const bool in = k0 + word * 8 < p.k;
+            const char* w = reinterpret_cast<const char*>(kGated && i >= 2 ? p.w2 + n0 * p.w2_stride
+                                                                           : p.w + n0 * p.w_stride);
+            const char* x = reinterpret_cast<const char*>(p.x + m0 * p.x_stride);
+            x8 a = {}, b = {};
+            if (in) {
+                a = *reinterpret_cast<const x8*>(w + (uint32_t)woff[i] + (int64_t)k0 * 2);
+                b = *reinterpret_cast<const x8*>(x + (uint32_t)xoff[i] + (int64_t)k0 * 2);
+            }
+            *reinterpret_cast<x8*>(ws0 + r * kTileK + lane % 8 * 8) = a;
+            *reinterpret_cast<x8*>(xs0 + r * kTileK + lane % 8 * 8) = b;
+        }
+        __syncthreads();
+        multiply(ws0, xs0);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; i += kGated ? 2 : 1)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t at = m0 + wm + j * 16 + row;
+                const int64_t c = n0 + (kGated ? (wn + i * 16) / 2 : wn + i * 16) + part * 4 + r;
+                if (at < p.m && c < p.n)
+                    put<T, kGated>(p, at, c, acc[i][j][r], acc[kGated ? i + 1 : i][j][r]);
+            }
+}
+
 struct Work {
     uint32_t* counters = nullptr;
     float* partial = nullptr;
@@ -436,6 +567,14 @@ void launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
     if (wide && p.m <= 32) return shared_groups<T, kGated, 2>(p, work, stream);
     if (wide && p.m <= 64) return shared_groups<T, kGated, 4>(p, work, stream);
     if (wide && p.m <= 128) return shared_groups<T, kGated, 8>(p, work, stream);
+    // a tile's rows are addressed in 32 bits
+    const bool near = std::max({p.x_stride, p.w_stride, p.w2_stride}) < (1 << 21);
+    if (wide && near) {
+        const int cols = kGated ? kTile / 2 : kTile;
+        const int tm = (p.m + kTile - 1) / kTile, tn = (p.n + cols - 1) / cols;
+        linear_tile<T, kGated><<<tm * tn, kTileWaves * 64, 0, stream>>>(p, tm, tn);
+        return;
+    }
     const dim3 grid((p.n + kElemTile - 1) / kElemTile, (p.m + kElemTile - 1) / kElemTile);
     linear_elements<T, kGated><<<grid, 256, 0, stream>>>(p);
 }
