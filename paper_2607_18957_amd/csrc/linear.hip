@@ -1,5 +1,6 @@
 // ii_linear: products with weight matrices, and their epilogue.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 #include "ops_device.h"
@@ -14,12 +15,26 @@ struct Linear {
     int64_t x_stride, w_stride, w2_stride, residual_stride, out_stride;
     int32_t m, n, k, act;
     bool out_f32;
+    bool quads;  // four columns of out, biases and residual at a time
 };
+
+// y / (1 + exp(-y)). The exponent's product is kept in two parts, so that the
+// result is right to some units in the last place however negative y is; the
+// reciprocal is the hardware's (1 unit): the division took 5% of a large gated
+// product's time.
+__device__ inline float silu(float y) {
+    constexpr float kHigh = -1.44269504f, kLow = -1.92596299e-8f;  // -log2(e)
+    // past 2^126 the quotient is below the normal range: 0, as at infinity
+    const float x = __builtin_amdgcn_fmed3f(y, -200.0f, 200.0f);
+    const float t = x * kHigh, rest = fmaf(x, kHigh, -t) + x * kLow;
+    const float e = __builtin_amdgcn_exp2f(t) * fmaf(rest, 0.693147181f, 1.0f);
+    return y * __builtin_amdgcn_rcpf(1.0f + e);
+}
 
 __device__ inline float activate(float y, int act) {
     switch (act) {
     case II_ACT_RELU: return y < 0 ? 0.0f : y;  // NaN stays
-    case II_ACT_SILU: return y / (1.0f + expf(-y));
+    case II_ACT_SILU: return silu(y);
     case II_ACT_GELU: return 0.5f * y * (1.0f + erff(y * 0.70710678118654752f));
     }
     return y;
@@ -40,52 +55,57 @@ __device__ inline void put(const Linear<T>& p, int64_t i, int64_t j, float y, fl
         static_cast<T*>(p.out)[i * p.out_stride + j] = (T)y;
 }
 
-// 64 tokens by 64 weight rows a workgroup of four waves, 32 elements of k at
-// a time through LDS, every element loaded by itself: rows at any address.
-constexpr int kElemTile = 64, kElemK = 32, kElemPad = 8;
-
-template <class T>
-__device__ inline void stage_elements(T (*to)[kElemK + kElemPad], const T* from, int64_t stride,
-                                      int64_t row0, int64_t rows, int64_t k0, int64_t k) {
-    const int t = threadIdx.x, r = t / 4, c = t % 4 * 8;
+// Columns j .. j + 3 of row i, j a multiple of 4.
+template <class T, bool kGated>
+__device__ inline void put4(const Linear<T>& p, int64_t i, int64_t j, f32x4 y, f32x4 z) {
+    using x4 = typename Vec<T>::x4;
+    if (!p.quads || j + 4 > p.n) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        T v = (T)0.0f;
-        if (row0 + r < rows && k0 + c + j < k) v = from[(row0 + r) * stride + k0 + c + j];
-        to[r][c + j] = v;
+        for (int r = 0; r < 4; ++r)
+            if (j + r < p.n) put<T, kGated>(p, i, j + r, y[r], z[r]);
+        return;
+    }
+    const auto add = [](f32x4& to, const T* from) {
+        const x4 v = *reinterpret_cast<const x4*>(from);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) to[r] += (float)v[r];
+    };
+    if (p.bias) add(y, p.bias + j);
+    if (p.act != II_ACT_NONE)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = activate(y[r], p.act);
+    if (kGated) {
+        if (p.bias2) add(z, p.bias2 + j);
+        y *= z;
+    }
+    if (p.residual) add(y, p.residual + i * p.residual_stride + j);
+    if (p.out_f32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + i * p.out_stride + j) = y;
+    } else {
+        x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = (T)y[r];
+        *reinterpret_cast<x4*>(static_cast<T*>(p.out) + i * p.out_stride + j) = v;
     }
 }
 
-template <class T, bool kGated>
-__global__ __launch_bounds__(256) void linear_elements(Linear<T> p) {
-    using x8 = typename Vec<T>::x8;
-    __shared__ T xs[kElemTile][kElemK + kElemPad];
-    __shared__ T ws[kGated ? 2 : 1][kElemTile][kElemK + kElemPad];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
-    const int64_t n0 = (int64_t)blockIdx.x * kElemTile, m0 = (int64_t)blockIdx.y * kElemTile;
-    f32x4 acc[kGated ? 2 : 1][4] = {};
-    for (int64_t k0 = 0; k0 < p.k; k0 += kElemK) {
-        stage_elements(xs, p.x, p.x_stride, m0, p.m, k0, p.k);
-        stage_elements(ws[0], p.w, p.w_stride, n0, p.n, k0, p.k);
-        if (kGated) stage_elements(ws[kGated], p.w2, p.w2_stride, n0, p.n, k0, p.k);
-        __syncthreads();
-#pragma unroll
-        for (int g = 0; g <= (kGated ? 1 : 0); ++g) {
-            const x8 a = *reinterpret_cast<const x8*>(&ws[g][wave * 16 + row][part * 8]);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                acc[g][t] = mfma16(a, *reinterpret_cast<const x8*>(&xs[t * 16 + row][part * 8]),
-                                   acc[g][t]);
-        }
-        __syncthreads();
+// The sums of the gridDim.y workgroups of a tile, kSums of each in red, joined
+// in red of the last of them; false in the others.
+template <int kSums, int kThreads>
+__device__ inline bool join(float* red, uint32_t* counters, float* partial) {
+    const Rsrc parts = buffer(partial + (int64_t)blockIdx.x * gridDim.y * kSums,
+                              (int64_t)gridDim.y * kSums * 4);
+    __syncthreads();
+    for (int e = threadIdx.x * 4; e < kSums; e += kThreads * 4)
+        leave_part(parts, (blockIdx.y * kSums + e) * 4, *reinterpret_cast<f32x4*>(&red[e]));
+    if (!arrive_last(&counters[blockIdx.x], gridDim.y)) return false;
+    for (int e = threadIdx.x * 4; e < kSums; e += kThreads * 4) {
+        f32x4 s = {};
+#pragma unroll 4
+        for (uint32_t y = 0; y < gridDim.y; ++y) s += take_part(parts, (y * kSums + e) * 4);
+        *reinterpret_cast<f32x4*>(&red[e]) = s;
     }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t i = m0 + t * 16 + row, j = n0 + wave * 16 + part * 4 + r;
-            if (i < p.m && j < p.n) put<T, kGated>(p, i, j, acc[0][t][r], acc[kGated][t][r]);
-        }
+    return true;
 }
 
 // Few tokens: the weights are read once, straight into the matrix
@@ -103,7 +123,7 @@ __global__ __launch_bounds__(kWaves * 64) void linear_stream(Linear<T> p, uint32
     using x8 = typename Vec<T>::x8;
     constexpr int kSets = kGated ? 2 : 1, kMine = kRows * 16 / kSets;  // rows of each matrix
     constexpr int kSums = kRows * kTokens * 256;
-    __shared__ float red[kWaves * kSums];
+    __shared__ __attribute__((aligned(16))) float red[kWaves * kSums];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
     const int64_t n0 = (int64_t)blockIdx.x * kMine;
     const int units = (p.k + kUnit - 1) / kUnit, whole = p.k / kUnit;
@@ -179,19 +199,8 @@ __global__ __launch_bounds__(kWaves * 64) void linear_stream(Linear<T> p, uint32
         for (int w = 1; w < kWaves; ++w) s += red[w * kSums + e];
         red[e] = s;
     }
-    if (gridDim.y > 1) {
-        float* mine = partial + ((int64_t)blockIdx.x * gridDim.y + blockIdx.y) * kSums;
-        for (int e = threadIdx.x; e < kSums; e += kWaves * 64) leave_part(&mine[e], red[e]);
-        if (!arrive_last(&counters[blockIdx.x], gridDim.y)) return;
-        const float* all = partial + (int64_t)blockIdx.x * gridDim.y * kSums;
-        for (int e = threadIdx.x; e < kSums; e += kWaves * 64) {
-            float s = 0;
-            for (uint32_t y = 0; y < gridDim.y; ++y) s += take_part(&all[(int64_t)y * kSums + e]);
-            red[e] = s;
-        }
-    }
-    // with a gate a thread's y and z lie kSums / 2 apart: another thread's sums
-    if (kGated) __syncthreads();
+    if (gridDim.y > 1 && !join<kSums, kWaves * 64>(red, counters, partial)) return;
+    __syncthreads();
     for (int e = threadIdx.x; e < kSums / kSets; e += kWaves * 64) {
         const int r = e / (kTokens * 256), i = e / 16 % (kTokens * 16);
         const int64_t j = n0 + r * 16 + e % 16;
@@ -204,12 +213,13 @@ __global__ __launch_bounds__(kWaves * 64) void linear_stream(Linear<T> p, uint32
 // waves of a k group share them; each wave owns 16 weight rows (with a gate 16
 // of w and 16 of w2), kKGroups groups of waves and gridDim.y workgroups share
 // k. Weights are requested two chunks ahead of their use, x one.
+constexpr int kRowWaves = 2, kKGroups = 8;
 constexpr int kChunkPad = 8;         // LDS rows 16 bytes apart in banks
 
 // elements of k a group takes at once
 constexpr int shared_chunk(bool gated) { return gated ? 64 : 128; }
 
-template <class T, bool kGated, int kTokens, int kRowWaves, int kKGroups>
+template <class T, bool kGated, int kTokens>
 __global__ __launch_bounds__(kRowWaves * kKGroups * 64) void linear_shared(Linear<T> p,
                                                                            uint32_t* counters,
                                                                            float* partial) {
@@ -325,17 +335,7 @@ __global__ __launch_bounds__(kRowWaves * kKGroups * 64) void linear_shared(Linea
             for (int g = 1; g < kKGroups; ++g) s += red[g * kAll + e];
             red[e] = s;
         }
-    if (gridDim.y > 1) {
-        float* mine = partial + ((int64_t)blockIdx.x * gridDim.y + blockIdx.y) * kAll;
-        for (int e = threadIdx.x; e < kAll; e += kThreads) leave_part(&mine[e], red[e]);
-        if (!arrive_last(&counters[blockIdx.x], gridDim.y)) return;
-        const float* all = partial + (int64_t)blockIdx.x * gridDim.y * kAll;
-        for (int e = threadIdx.x; e < kAll; e += kThreads) {
-            float s = 0;
-            for (uint32_t y = 0; y < gridDim.y; ++y) s += take_part(&all[(int64_t)y * kAll + e]);
-            red[e] = s;
-        }
-    }
+    if (gridDim.y > 1 && !join<kAll, kThreads>(red, counters, partial)) return;
     __syncthreads();
     // lanes along a token's columns
     constexpr int kCols = kRowWaves * 16, kOut = kCols * kTokens * 16;
@@ -348,136 +348,300 @@ __global__ __launch_bounds__(kRowWaves * kKGroups * 64) void linear_shared(Linea
     }
 }
 
-// Many tokens: 256 tokens by 256 weight rows (with a gate 128 of w and 128 of
-// w2, in turn by 16) a workgroup of eight waves, each 128 tokens by 64 rows.
-// Both operands go from memory straight into LDS, 64 elements of k at a time,
-// the next ones while these are multiplied. An LDS row is 128 bytes, its
-// 16-byte words exchanged by the row's last three bits, so that the eight
-// lanes of one LDS cycle, a row each, meet all banks.
-constexpr int kTile = 256, kTileK = 64, kTileWaves = 8;
+// Many tokens: kTile tokens by kTile weight rows (with a gate half of them of
+// w2, in turn by 16) a workgroup of eight waves, each kTile / 2 tokens by
+// kTile / 4 rows. Both operands go from memory straight into LDS, 64 elements
+// of k at a time, the next ones while these are multiplied. An LDS row is 128
+// bytes, its 16-byte words exchanged by the row's last three bits, so that the
+// eight lanes of one LDS cycle, a row each, meet all banks. A workgroup goes
+// on to its next tile's first words before it writes a tile. Few tiles share k
+// among gridDim.y workgroups, which leave their sums in `partial`.
+constexpr int kTileK = 64, kTileWaves = 8;
 
-using Rsrc = __amdgpu_buffer_rsrc_t;
-
-__device__ inline Rsrc rows_rsrc(const void* base, int64_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0,
-                                             (int)(uint32_t)min(bytes, (int64_t)0xffffffffll),
-                                             0x00020000);
+// 16 bytes a lane from r at offset + step into LDS, the wave's 1024 in a row.
+__device__ inline void load_lds16(Rsrc r, void* lds, int offset, int step) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16,
+                                             offset, step, 0, 0);
 }
 
-template <class T, bool kGated>
-__global__ __launch_bounds__(kTileWaves * 64) void linear_tile(Linear<T> p, int tiles_m,
-                                                               int tiles_n) {
+// One LDS buffer of a stage; each is a variable of its own, so that the
+// compiler can tell reads of one from loads into another.
+template <class T, int kStage, int kOperand, int kRows>
+__device__ inline T* stage_rows() {
+    __shared__ __attribute__((aligned(1024))) T rows[kRows * kTileK];
+    return rows;
+}
+
+template <int kValue>
+struct Int {
+    static constexpr int value = kValue;
+};
+// f(Int<0>), f(Int<1>), .. f(Int<kN - 1>)
+template <int kN, int kI = 0, class F>
+__device__ inline void each_of(F&& f) {
+    if constexpr (kI < kN) {
+        f(Int<kI>{});
+        each_of<kN, kI + 1>(f);
+    }
+}
+
+// All but kYounger of this wave's last memory instructions done, its LDS reads
+// too; then every wave of the workgroup.
+template <int kYounger>
+__device__ inline void meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kYounger) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <class T, bool kGated, int kM, int kN, int kStages, bool kDirect>
+__global__ __launch_bounds__(kTileWaves * 64, kM * kN == 256 * 256 ? 2 : 4) void linear_tile(
+    Linear<T> p, int tiles_m, int tiles_n, uint32_t* counters, float* partial) {
     using x8 = typename Vec<T>::x8;
-    __shared__ __attribute__((aligned(1024))) T ws0[kTile * kTileK];
-    __shared__ __attribute__((aligned(1024))) T ws1[kTile * kTileK];
-    __shared__ __attribute__((aligned(1024))) T xs0[kTile * kTileK];
-    __shared__ __attribute__((aligned(1024))) T xs1[kTile * kTileK];
+    // instructions of a wave that bring an operand, 8 rows each
+    constexpr int kBringW = kN / 64, kBringX = kM / 64;
+    constexpr int kA = kN / 64, kB = kM / 32;  // a wave's fragments of 16 rows
+    static_assert(!kGated || kA % 2 == 0);
+    constexpr int kCols = kGated ? kN / 2 : kN;  // columns of out
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int row = lane % 16, part = lane / 16;
+    const int wn = wave % 4 * (kN / 4), wm = wave / 4 * (kM / 2);
 
-    // workgroups go to the 8 XCDs in turn: each XCD gets a run of tiles, in
+    // Workgroups go to the 8 XCDs in turn: each XCD gets a run of tiles, in
     // bands of 4 tiles of tokens, so that the tiles its L2 serves at one time
-    // share rows
-    const int total = tiles_m * tiles_n, xcd = blockIdx.x % 8, place = blockIdx.x / 8;
-    const int tile = xcd * (total / 8) + min(xcd, total % 8) + place;
+    // share rows.
     constexpr int kBand = 4;
-    const int band = tile / (kBand * tiles_n), in_band = tile % (kBand * tiles_n);
-    const int high = min(kBand, tiles_m - band * kBand);
-    const int tm = band * kBand + in_band % high, tn = in_band / high;
+    const int total = tiles_m * tiles_n, xcd = blockIdx.x % 8;
+    const int begin = xcd * (total / 8) + min(xcd, total % 8);
+    const int end = begin + total / 8 + (xcd < total % 8);
+    const int stride = (gridDim.x - xcd + 7) / 8;  // workgroups of this XCD
+    int tile = begin + blockIdx.x / 8;
+    if (tile >= end) return;
 
-    constexpr int kCols = kGated ? kTile / 2 : kTile;  // columns of out
-    const int64_t m0 = (int64_t)tm * kTile, n0 = (int64_t)tn * kCols;
+    // this workgroup's part of k, in steps; the last part has the rest
+    const int steps_all = p.k / kTileK, each = (steps_all + gridDim.y - 1) / gridDim.y;
+    const int step0 = min((int)blockIdx.y * each, steps_all);
+    const int steps = min(each, steps_all - step0);
+    const int64_t k0 = (int64_t)step0 * kTileK;
+    const bool rest = p.k % kTileK && blockIdx.y == gridDim.y - 1;
 
-    // what this wave brings: 32 rows of each operand, 8 rows an instruction
-    const int64_t n_end = p.n - 1 - n0, m_end = p.m - 1 - m0;
-    const Rsrc wr = rows_rsrc(p.w + n0 * p.w_stride, (n_end * p.w_stride + p.k) * 2);
-    const Rsrc w2r = kGated ? rows_rsrc(p.w2 + n0 * p.w2_stride, (n_end * p.w2_stride + p.k) * 2) : wr;
-    const Rsrc xr = rows_rsrc(p.x + m0 * p.x_stride, (m_end * p.x_stride + p.k) * 2);
-    int woff[4], xoff[4];
+    // what this wave brings of a tile: an eighth of the rows of each operand
+    int64_t m0, n0;
+    const T *wbase, *xbase;
+    Rsrc wr, xr;
+    using Offset = std::conditional_t<kDirect, int, int64_t>;
+    Offset woff[kBringW], xoff[kBringX];
+    // with a gate, a tile's weight rows are 16 by 16 of w and of w2
+    auto mat = [&](int i) { return kGated && (wave * (kN / 8) + i * 8) / 16 % 2; };
+    const T* w2base = nullptr;
+    Rsrc w2r;
+    auto place = [&]() {
+        const int band = tile / (kBand * tiles_n), in_band = tile % (kBand * tiles_n);
+        const int high = min(kBand, tiles_m - band * kBand);
+        m0 = (int64_t)(band * kBand + in_band % high) * kM;
+        n0 = (int64_t)(in_band / high) * kCols;
+        const int64_t n_end = p.n - 1 - n0, m_end = p.m - 1 - m0, k = p.k - k0;
+        wbase = p.w + n0 * p.w_stride + k0;
+        xbase = p.x + m0 * p.x_stride + k0;
+        wr = buffer(wbase, (n_end * p.w_stride + k) * 2);
+        xr = buffer(xbase, (m_end * p.x_stride + k) * 2);
+        if (kGated) {
+            w2base = p.w2 + n0 * p.w2_stride + k0;
+            w2r = buffer(w2base, (n_end * p.w2_stride + k) * 2);
+        }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = wave * 32 + i * 8 + lane / 8, word = (lane % 8) ^ (r % 8);
-        const int64_t c = kGated ? r / 32 * 16 + r % 16 : r;
-        const int64_t stride = kGated && i >= 2 ? p.w2_stride : p.w_stride;
-        woff[i] = (int)((min(c, n_end) * stride + word * 8) * 2);
-        xoff[i] = (int)((min((int64_t)r, m_end) * p.x_stride + word * 8) * 2);
-    }
-    auto bring = [&](int k, T* ws, T* xs) {
+        for (int i = 0; i < kBringW; ++i) {
+            const int r = wave * (kN / 8) + i * 8 + lane / 8, word = (lane % 8) ^ (r % 8);
+            const int64_t c = kGated ? r / 32 * 16 + r % 16 : r;
+            const int64_t s = mat(i) ? p.w2_stride : p.w_stride;
+            woff[i] = (Offset)((min(c, n_end) * s + word * 8) * 2);
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                kGated && i >= 2 ? w2r : wr,
-                (__attribute__((address_space(3))) void*)(ws + (wave * 32 + i * 8) * kTileK), 16,
-                woff[i], k * 2, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                xr, (__attribute__((address_space(3))) void*)(xs + (wave * 32 + i * 8) * kTileK), 16,
-                xoff[i], k * 2, 0, 0);
+        for (int i = 0; i < kBringX; ++i) {
+            const int r = wave * (kM / 8) + i * 8 + lane / 8, word = (lane % 8) ^ (r % 8);
+            xoff[i] = (Offset)((min((int64_t)r, m_end) * p.x_stride + word * 8) * 2);
         }
     };
-    const int wn = wave % 4 * 64, wm = wave / 4 * 128;
-    f32x4 acc[4][8] = {};
-    auto multiply = [&](const T* ws, const T* xs) {
+    constexpr int kLoads = kBringW + kBringX;
+    // stage i of the ring <- elements k .. of this part
+    auto bring = [&](int k, auto i_) {
+        T* const ws = stage_rows<T, i_.value, 0, kN>();
+        T* const xs = stage_rows<T, i_.value, 1, kM>();
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            x8 a[4], b[8];
-            const int word = ((s * 4 + part) ^ (row % 8)) * 8;
+        for (int i = 0; i < kBringW; ++i) {
+            const int at = (wave * (kN / 8) + i * 8) * kTileK;
+            if (kGated && mat(i))
+                load_lds16(w2r, ws + at, (int)woff[i], k * 2);
+            else
+                load_lds16(wr, ws + at, (int)woff[i], k * 2);
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                a[i] = *reinterpret_cast<const x8*>(ws + (wn + i * 16 + row) * kTileK + word);
+        for (int i = 0; i < kBringX; ++i)
+            load_lds16(xr, xs + (wave * (kM / 8) + i * 8) * kTileK, (int)xoff[i], k * 2);
+    };
+    // the same in two halves: into registers from any address, words past the
+    // end of k zero, then into LDS
+    x8 held[kLoads];
+    auto fetch = [&](int k) {
+        const int64_t at = k0 + k + (lane % 8 ^ lane / 8) * 8;  // of this lane's words
+        const auto word = [&](const T* base, int64_t off) {
+            const char* from = reinterpret_cast<const char*>(base) + off + (int64_t)k * 2;
+            if (kDirect) return at < p.k ? *reinterpret_cast<const x8*>(from) : x8{};
+            x8 v = {};
+            if (at + 8 <= p.k) {
+                __builtin_memcpy(&v, from, 16);
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                b[j] = *reinterpret_cast<const x8*>(xs + (wm + j * 16 + row) * kTileK + word);
+                for (int e = 0; e < 7; ++e)
+                    if (at + e < p.k) v[e] = reinterpret_cast<const T*>(from)[e];
+            }
+            return v;
+        };
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+        for (int i = 0; i < kBringW; ++i) held[i] = word(mat(i) ? w2base : wbase, woff[i]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i][j] = mfma16(a[i], b[j], acc[i][j]);
+        for (int i = 0; i < kBringX; ++i) held[kBringW + i] = word(xbase, xoff[i]);
+    };
+    auto keep = [&](auto i_) {
+        T* const ws = stage_rows<T, i_.value, 0, kN>();
+        T* const xs = stage_rows<T, i_.value, 1, kM>();
+#pragma unroll
+        for (int i = 0; i < kBringW; ++i)
+            *reinterpret_cast<x8*>(ws + (wave * (kN / 8) + i * 8) * kTileK + lane * 8) = held[i];
+#pragma unroll
+        for (int i = 0; i < kBringX; ++i)
+            *reinterpret_cast<x8*>(xs + (wave * (kM / 8) + i * 8) * kTileK + lane * 8) =
+                held[kBringW + i];
+    };
+    auto begin_tile = [&]() {
+        place();
+        if constexpr (kDirect) {
+            each_of<kStages - 1>([&](auto i_) {
+                if (i_.value < steps) bring(i_.value * kTileK, i_);
+            });
+        } else if (steps > 0) {
+            fetch(0);
+            keep(Int<0>{});
         }
     };
-    const int steps = p.k / kTileK;
-    if (steps > 0) bring(0, ws0, xs0);
-    for (int t = 0; t < steps; t += 2) {
-        __syncthreads();
-        if (t + 1 < steps) bring((t + 1) * kTileK, ws1, xs1);
-        multiply(ws0, xs0);
-        if (t + 1 < steps) {
-            __syncthreads();
-            if (t + 2 < steps) bring((t + 2) * kTileK, ws0, xs0);
-            multiply(ws1, xs1);
-        }
-    }
-    if (p.k % kTileK) {  // the rest of k: words past it are zero
-        __syncthreads();
-        const int k0 = steps * kTileK;
+    begin_tile();
+    for (;;) {
+        f32x4 acc[kA][kB] = {};
+        auto multiply = [&](auto i_) {
+            const T* const ws = stage_rows<T, i_.value, 0, kN>();
+            const T* const xs = stage_rows<T, i_.value, 1, kM>();
+            x8 a[2][kA], b[2][kB];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = wave * 32 + i * 8 + lane / 8, word = (lane % 8) ^ (r % 8);
-            const bool in = k0 + word * 8 < p.k;
-            const char* w = reinterpret_cast<const char*>(kGated && i >= 2 ? p.w2 + n0 * p.w2_stride
-                                                                           : p.w + n0 * p.w_stride);
-            const char* x = reinterpret_cast<const char*>(p.x + m0 * p.x_stride);
-            x8 a = {}, b = {};
-            if (in) {
-                a = *reinterpret_cast<const x8*>(w + (uint32_t)woff[i] + (int64_t)k0 * 2);
-                b = *reinterpret_cast<const x8*>(x + (uint32_t)xoff[i] + (int64_t)k0 * 2);
+            for (int s = 0; s < 2; ++s) {
+                const int word = ((s * 4 + part) ^ (row % 8)) * 8;
+#pragma unroll
+                for (int i = 0; i < kA; ++i)
+                    a[s][i] = *reinterpret_cast<const x8*>(ws + (wn + i * 16 + row) * kTileK + word);
+#pragma unroll
+                for (int j = 0; j < kB; ++j)
+                    b[s][j] = *reinterpret_cast<const x8*>(xs + (wm + j * 16 + row) * kTileK + word);
             }
-            *reinterpret_cast<x8*>(ws0 + r * kTileK + lane % 8 * 8) = a;
-            *reinterpret_cast<x8*>(xs0 + r * kTileK + lane % 8 * 8) = b;
-        }
-        __syncthreads();
-        multiply(ws0, xs0);
-    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int i = 0; i < 4; i += kGated ? 2 : 1)
+                for (int j = 0; j < kB; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t at = m0 + wm + j * 16 + row;
-                const int64_t c = n0 + (kGated ? (wn + i * 16) / 2 : wn + i * 16) + part * 4 + r;
-                if (at < p.m && c < p.n)
-                    put<T, kGated>(p, at, c, acc[i][j][r], acc[kGated ? i + 1 : i][j][r]);
+                    for (int i = 0; i < kA; ++i) acc[i][j] = mfma16(a[s][i], b[s][j], acc[i][j]);
+            // the first half's reads, then the second's among the first's products
+            constexpr int kReads = kA + kB, kProducts = kA * kB;
+            __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+#pragma unroll
+            for (int i = 0; i < kReads; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, kProducts >= 2 * kReads ? 2 : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
+            __builtin_amdgcn_sched_group_barrier(0x008, 2 * kProducts, 0);
+        };
+        for (int t0 = 0; t0 < steps; t0 += kStages) {
+            each_of<kStages>([&](auto i_) {
+                const int t = t0 + i_.value;
+                if (t >= steps) return;
+                if constexpr (!kDirect) {
+                    meet<0>();
+                    if (t + 1 < steps) fetch((t + 1) * kTileK);
+                    multiply(i_);
+                    if (t + 1 < steps) keep(Int<(i_.value + 1) % kStages>{});
+                    return;
+                }
+                // the loads of this step are older than those of the next ones
+                if (t + kStages - 2 < steps)
+                    meet<(kStages - 2) * kLoads>();
+                else
+                    meet<0>();
+                // into the stage that every wave has multiplied
+                if (t + kStages - 1 < steps)
+                    bring((t + kStages - 1) * kTileK, Int<(i_.value + kStages - 1) % kStages>{});
+                multiply(i_);
+            });
+        }
+        if (rest) {  // what is left of k
+            meet<0>();
+            fetch(steps * kTileK);
+            keep(Int<0>{});
+            meet<0>();
+            multiply(Int<0>{});
+        }
+        const int64_t m_out = m0 + wm, n_out = n0 + (kGated ? wn / 2 : wn);
+        const int done = tile;
+        tile += stride;
+        if (tile < end) {
+            meet<0>();
+            begin_tile();
+        }
+        bool mine = true;
+        if (gridDim.y > 1) {
+            constexpr int64_t kSums = (int64_t)kM * kN;
+            const Rsrc parts = buffer(partial + (int64_t)done * gridDim.y * kSums,
+                                      (int64_t)gridDim.y * kSums * 4);
+            const auto offset = [&](uint32_t y, int i, int j) {
+                return (uint32_t)(y * kSums + ((i * kB + j) * kTileWaves * 64 + threadIdx.x) * 4) * 4;
+            };
+#pragma unroll
+            for (int i = 0; i < kA; ++i)
+#pragma unroll
+                for (int j = 0; j < kB; ++j)
+                    leave_part(parts, offset(blockIdx.y, i, j), acc[i][j]);
+            mine = arrive_last(&counters[done], gridDim.y);
+            if (mine) {
+#pragma unroll
+                for (int i = 0; i < kA; ++i)
+#pragma unroll
+                    for (int j = 0; j < kB; ++j) acc[i][j] = f32x4{};
+                // a part at a time, its loads under way together
+#pragma unroll(kA * kB < 16 ? 4 : 1)
+                for (uint32_t y = 0; y < gridDim.y; ++y) {
+                    f32x4 v[kA][kB];
+#pragma unroll
+                    for (int i = 0; i < kA; ++i)
+#pragma unroll
+                        for (int j = 0; j < kB; ++j) v[i][j] = take_part(parts, offset(y, i, j));
+#pragma unroll
+                    for (int i = 0; i < kA; ++i)
+#pragma unroll
+                        for (int j = 0; j < kB; ++j) acc[i][j] += v[i][j];
+                }
+            }
+        }
+        if (mine) {
+#pragma unroll
+            for (int j = 0; j < kB; ++j)
+#pragma unroll
+                for (int i = 0; i < kA; i += kGated ? 2 : 1) {
+                    const int64_t at = m_out + j * 16 + row;
+                    const int64_t c = n_out + (kGated ? i * 8 : i * 16) + part * 4;
+                    if (at < p.m) put4<T, kGated>(p, at, c, acc[i][j], acc[kGated ? i + 1 : i][j]);
+                }
+        }
+        if (tile >= end) break;
+    }
 }
+
+constexpr uint32_t kUnits = 256;  // compute units
 
 struct Work {
     uint32_t* counters = nullptr;
@@ -512,7 +676,7 @@ void stream_waves(const Linear<T>& p, const Work& work, hipStream_t stream) {
         stream_launch<T, kGated, kRows, kTokens, 4, kAhead>(p, work, stream);
 }
 
-template <class T, bool kGated, int kTokens, int kRowWaves, int kKGroups>
+template <class T, bool kGated, int kTokens>
 void shared_launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
     constexpr int kCols = kRowWaves * 16;
     constexpr uint64_t kAll = (uint64_t)kCols * kTokens * 16 * (kGated ? 2 : 1);
@@ -520,34 +684,63 @@ void shared_launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
     const uint32_t chunks = (p.k + shared_chunk(kGated) - 1) / shared_chunk(kGated);
     // as many workgroups as compute units, each wave with a chunk or more
     uint32_t split = 1;
-    if (work.partial && tiles < 256)
-        split = std::max(1u, std::min(256 / tiles, (chunks + kKGroups - 1) / kKGroups));
+    if (work.partial && tiles < kUnits)
+        split = std::max(1u, std::min(kUnits / tiles, (chunks + kKGroups - 1) / kKGroups));
     while (split > 1 && tiles * split * kAll > work.floats) --split;
-    linear_shared<T, kGated, kTokens, kRowWaves, kKGroups>
-        <<<dim3(tiles, split), kRowWaves * kKGroups * 64, 0, stream>>>(p, work.counters,
-                                                                       work.partial);
+    linear_shared<T, kGated, kTokens><<<dim3(tiles, split), kRowWaves * kKGroups * 64, 0, stream>>>(
+        p, work.counters, work.partial);
 }
 
-// A workgroup a compute unit with all the waves it takes, or two of half as
-// many where there are rows enough. Measured at 24 x 4096 x 14336 (256
-// workgroups in all): 16 waves by 32 rows 30.7 us, by 64 rows 31.4, 8 waves by
-// 32 rows and twice the workgroups 34.5; at 8 x 128256 x 4096: 8 waves by 64
-// rows 191 us, 16 waves 215, 4 waves 202; with a gate at 24 x 14336 x 4096: 8
-// waves by 32 rows 52.6 us, by 64 rows 58.8, 16 waves by 64 rows 57.0.
-template <class T, bool kGated, int kTokens>
-void shared_groups(const Linear<T>& p, const Work& work, hipStream_t stream) {
-    if constexpr (kTokens <= 2) {
-        if ((p.n + 31) / 32 <= 256)
-            return shared_launch<T, kGated, kTokens, 2, 8>(p, work, stream);
+// A tile shape, over how many workgroups a tile's k is split, and the time in
+// us that the pair is expected to take: a step of 64 elements of k takes each
+// shape so long with a workgroup a compute unit; joining costs its start and
+// the reading of the parts by the workgroup that comes last, at 60 GB/s.
+// Measured: 128 x 4096 x 4096 by 64 x 128 in 4 parts 18.7 us (expected 18);
+// 256 x 4096 x 4096 the same in 2 parts 23.7 (24); 1024 x 4096 x 4096 by
+// 128 x 256 in 2 parts 48 (44), by 64 x 128 54 (68); 512 x 4096 x 14336 by
+// 128 x 256 in 4 parts 86 (74); 512 x 14336 x 4096 with a gate by 256 x 256
+// 114 (110), by 128 x 256 128 (138).
+struct Shape {
+    int m, n;
+    double step;
+    bool splits;  // 256 x 256 has too much to join
+};
+constexpr Shape kShapes[3] = {{64, 128, 0.5, true}, {128, 256, 1.05, true}, {256, 256, 1.65, false}};
+struct Choice {
+    int shape = 0;
+    uint32_t split = 1;
+    double us = 1e30;
+};
+Choice choose_tile(int64_t m, int64_t n, int64_t k, bool gated, const Work& work, int shapes) {
+    Choice best;
+    const int64_t steps = (k + kTileK - 1) / kTileK;
+    for (int i = 0; i < shapes; ++i) {
+        const Shape& s = kShapes[i];
+        const int64_t cols = gated ? s.n / 2 : s.n;
+        const int64_t tiles = ((m + s.m - 1) / s.m) * ((n + cols - 1) / cols);
+        for (int64_t split = 1; split <= 16; ++split) {
+            if (split > 1 && (!s.splits || !work.partial || tiles * split > kUnits ||
+                              split * 2 > steps ||
+                              tiles * split * s.m * s.n > (int64_t)work.floats))
+                break;
+            const int64_t rounds = (tiles * split + kUnits - 1) / kUnits;
+            double us = rounds * ((steps + split - 1) / split) * s.step;
+            if (split > 1) us += 2 + split * s.m * s.n * 4 / 60e3;
+            if (us < best.us) best = {i, (uint32_t)split, us};
+        }
     }
-    if constexpr (kTokens <= 4) {
-        if ((p.n + 63) / 64 <= (kGated ? 128 : 256))
-            return shared_launch<T, kGated, kTokens, 4, 4>(p, work, stream);
-    }
-    if constexpr (kGated && kTokens <= 2)
-        shared_launch<T, kGated, kTokens, 2, 4>(p, work, stream);
-    else
-        shared_launch<T, kGated, kTokens, 4, 2>(p, work, stream);
+    return best;
+}
+
+template <class T, bool kGated, int kM, int kN, int kStages, bool kDirect>
+void tile_launch(const Linear<T>& p, const Work& work, uint32_t split, hipStream_t stream) {
+    constexpr int kCols = kGated ? kN / 2 : kN;
+    const int tm = (p.m + kM - 1) / kM, tn = (p.n + kCols - 1) / kCols;
+    const int64_t tiles = (int64_t)tm * tn;
+    const int64_t resident = kM == 64 ? 2 * kUnits : kUnits;  // workgroups the card holds at once
+    linear_tile<T, kGated, kM, kN, kStages, kDirect>
+        <<<dim3((uint32_t)std::min(tiles, resident), split), kTileWaves * 64, 0, stream>>>(
+            p, tm, tn, work.counters, work.partial);
 }
 
 // Whether rows can be read in 16-byte words.
@@ -563,20 +756,23 @@ void launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
     // 25.0 us against 28.1 through LDS, 1 x 128256 x 4096 177 against 186; from
     // 8 tokens on it is 29.2 against 27.4, 212 against 191
     if (wide && p.m <= 4) return stream_waves<T, kGated, kGated ? 2 : 1, 1, 4>(p, work, stream);
-    if (wide && p.m <= 16) return shared_groups<T, kGated, 1>(p, work, stream);
-    if (wide && p.m <= 32) return shared_groups<T, kGated, 2>(p, work, stream);
-    if (wide && p.m <= 64) return shared_groups<T, kGated, 4>(p, work, stream);
-    if (wide && p.m <= 128) return shared_groups<T, kGated, 8>(p, work, stream);
+    // rows that waves share through LDS, where it takes all waves of the card
+    // to keep up with the memory and a tile's rows would be too few: 24 x 4096
+    // x 14336 31.4 us against 33.6 in tiles; 24 x 14336 x 4096 with a gate
+    // 52.6 against 46
+    if (wide && p.m <= 32 && p.n <= kRowWaves * 16 * (int)kUnits) {
+        if (p.m <= 16) return shared_launch<T, kGated, 1>(p, work, stream);
+        return shared_launch<T, kGated, 2>(p, work, stream);
+    }
     // a tile's rows are addressed in 32 bits
     const bool near = std::max({p.x_stride, p.w_stride, p.w2_stride}) < (1 << 21);
-    if (wide && near) {
-        const int cols = kGated ? kTile / 2 : kTile;
-        const int tm = (p.m + kTile - 1) / kTile, tn = (p.n + cols - 1) / cols;
-        linear_tile<T, kGated><<<tm * tn, kTileWaves * 64, 0, stream>>>(p, tm, tn);
-        return;
-    }
-    const dim3 grid((p.n + kElemTile - 1) / kElemTile, (p.m + kElemTile - 1) / kElemTile);
-    linear_elements<T, kGated><<<grid, 256, 0, stream>>>(p);
+    const Choice c = choose_tile(p.m, p.n, p.k, kGated, work, wide && near ? 3 : 2);
+    if (!wide || !near)
+        return c.shape ? tile_launch<T, kGated, 128, 256, 2, false>(p, work, c.split, stream)
+                       : tile_launch<T, kGated, 64, 128, 2, false>(p, work, c.split, stream);
+    if (c.shape == 0) return tile_launch<T, kGated, 64, 128, 3, true>(p, work, c.split, stream);
+    if (c.shape == 1) return tile_launch<T, kGated, 128, 256, 3, true>(p, work, c.split, stream);
+    tile_launch<T, kGated, 256, 256, 2, true>(p, work, c.split, stream);
 }
 
 template <class T>
@@ -599,11 +795,16 @@ int run(const ii_linear_args& a, hipStream_t stream) {
     p.k = (int32_t)a.k;
     p.act = a.act;
     p.out_f32 = a.out_dtype == II_F32;
+    const auto quad = [](const void* at, int64_t stride, int size) {
+        return !at || (reinterpret_cast<uintptr_t>(at) % (4 * size) == 0 && stride % 4 == 0);
+    };
+    p.quads = quad(p.out, p.out_stride, p.out_f32 ? 4 : 2) && quad(p.bias, 0, 2) &&
+              quad(p.bias2, 0, 2) && quad(p.residual, p.residual_stride, 2);
     Work work;
     if (a.work_bytes > kWorkHead) {
         work.counters = static_cast<uint32_t*>(a.work);
         work.partial = reinterpret_cast<float*>(static_cast<char*>(a.work) + kWorkHead);
-        work.floats = (a.work_bytes - kWorkHead) / 4;
+        work.floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
     }
     if (p.w2)
         launch<T, true>(p, work, stream);

@@ -53,18 +53,32 @@ __device__ inline f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+using Rsrc = __amdgpu_buffer_rsrc_t;
+
+// Memory from base on for buffer instructions, which take 32-bit offsets and
+// give zeros past its end.
+__device__ inline Rsrc buffer(const void* base, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0,
+                                             (int)(uint32_t)min(bytes, (int64_t)0xffffffffll),
+                                             0x00020000);
+}
+
 // Workgroups that share a result leave their parts in global memory; the last
 // to arrive joins them, in the order of their places. The workgroups run on
 // XCDs whose L2 caches do not see each other, so parts are written and read by
-// accesses of agent scope, which go past those caches. Nothing else passes
-// between the workgroups, so it is enough that a wave's writes have arrived
-// before it counts itself: a fence of agent scope would also write back the
-// whole L2, which took 130 us where 512 workgroups of a 20 us kernel did it.
-__device__ inline void leave_part(float* at, float v) {
-    __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// instructions of device scope (sc1), which go past those caches. Nothing else
+// passes between the workgroups, so it is enough that a wave's writes have
+// arrived before it counts itself: a fence of device scope would also write
+// back the whole L2, which took 130 us where 512 workgroups of a 20 us kernel
+// did it.
+constexpr int kDeviceScope = 16;
+__device__ inline void leave_part(Rsrc parts, uint32_t offset, f32x4 v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), parts, (int)offset, 0,
+                                           kDeviceScope);
 }
-__device__ inline float take_part(const float* at) {
-    return __hip_atomic_load(const_cast<float*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ inline f32x4 take_part(Rsrc parts, uint32_t offset) {
+    return __builtin_bit_cast(
+        f32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, (int)offset, 0, kDeviceScope));
 }
 // Whether this workgroup is the last of `parts`; the counter is zero again
 // then. Called by every thread, after the parts were left.
@@ -78,6 +92,7 @@ __device__ inline bool arrive_last(uint32_t* counter, uint32_t parts) {
             __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
+    asm volatile("" ::: "memory");  // parts are taken after this
     return before == parts - 1;
 }
 
