@@ -1,4 +1,5 @@
 // ii_attend: attention of new tokens over a paged key/value cache.
+#include <algorithm>
 #include <cmath>
 
 #include "ops.h"
@@ -20,91 +21,455 @@ struct Attend {
     float scale;
 };
 
-template <class T, bool kQuant>
-__device__ inline float kept(const Attend& p, const uint8_t* base, const uint8_t* scales,
-                             int64_t page, int head, int64_t row, int d) {
-    const uint8_t* at = base + page * p.page_stride + head * p.head_stride + row * p.token_stride;
-    if (!kQuant) return (float)reinterpret_cast<const T*>(at)[d];
-    const uint32_t e = scales[page * p.scale_page_stride + head * p.scale_head_stride +
-                              row * p.scale_token_stride + d / 32];
-    return __builtin_amdgcn_cvt_f32_fp8(at[d], 0) * __builtin_bit_cast(float, e ? e << 23 : 0x400000u);
-}
+// ---------------------------------------------------------------------------
+// What the kernels share. Scores are formed transposed, keys by queries
+// (S^T = K Q^T), and so is the result (O^T = V^T P^T): with 16 x 16 x 32
+// products a lane then holds, of one query (its lane mod 16), the scores of
+// keys 4 (lane / 16) + r of each 16, which are just the operand that the second
+// product takes, if the 32 keys of a step are numbered 4 by 4: no score
+// crosses lanes. V^T comes out of LDS by the transposing read, whose 16 lanes
+// give 4 keys each of 16 positions.
 
-// One wave a (row, query head): 64 keys at a time, a lane a key for the
-// scores, a lane a few positions for the values.
+constexpr int kStep = 32;  // keys a wave takes at once
+
+// 8 or 16 bytes of codes (8-bit) or values of one key, as loaded: kWords words
+// of 16 bytes a lane for a key of kDim elements, lane part (lane / 16) having
+// bytes 64 c + 16 part of word c.
 template <class T, bool kQuant, int kDim>
-__global__ __launch_bounds__(64) void attend_rows(Attend p) {
-    __shared__ float qs[kDim], ps[64];
-    __shared__ int64_t at[64];
-    const int lane = threadIdx.x, head = blockIdx.y, kv = head / p.group;
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        // the row's sequence
-        int64_t seq = row, first = row, end = row + 1;
-        if (p.q_start) {
-            seq = -1;
-            for (int b = 0; b < p.seqs; ++b)
-                if (p.q_start[b] <= row && row < p.q_start[b + 1]) {
-                    seq = b;
-                    first = p.q_start[b];
-                    end = p.q_start[b + 1];
-                }
+struct Loaded {
+    static constexpr int kWords = kDim * (kQuant ? 1 : 2) / 64;
+    u32x4 w[kWords];
+    uint32_t scale;  // all scales of the key
+};
+
+// Elements of a loaded key: fragment f of kDim / 32 holds the 8 positions
+// first_position<..>(f, part) .. + 8.
+template <bool kQuant>
+__device__ inline int first_position(int f, int part) {
+    return kQuant ? f / 2 * 64 + part * 16 + f % 2 * 8 : f * 32 + part * 8;
+}
+__device__ inline bf16x2 unpack(uint32_t codes, float scale, bf16x2, bool high) {
+    return high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true)
+                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
+}
+__device__ inline f16x2 unpack(uint32_t codes, float scale, f16x2, bool high) {
+    return high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, true)
+                : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, false);
+}
+template <class T, bool kQuant, int kDim>
+__device__ inline typename Vec<T>::x8 fragment(const Loaded<T, kQuant, kDim>& l, int f, int part) {
+    using x8 = typename Vec<T>::x8;
+    using x2 = typename Vec<T>::x2;
+    if constexpr (kQuant) {
+        const uint32_t e = l.scale >> ((f / 2 * 2 + part / 2) * 8) & 255;
+        const float scale = __builtin_bit_cast(float, e << 23);
+        x8 v;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t codes = l.w[f / 2][f % 2 * 2 + i];
+            const x2 lo = unpack(codes, scale, x2{}, false), hi = unpack(codes, scale, x2{}, true);
+            v[i * 4] = lo[0];
+            v[i * 4 + 1] = lo[1];
+            v[i * 4 + 2] = hi[0];
+            v[i * 4 + 3] = hi[1];
         }
-        if (seq < 0 || seq >= p.seqs) continue;
-        const int64_t pos = (int64_t)p.lengths[seq] - (end - first) + (row - first);
-        const int64_t stop = min(pos + 1, p.capacity);
-        const int64_t start = p.window ? max((int64_t)0, pos - p.window + 1) : 0;
-        const T* q = reinterpret_cast<const T*>(p.q + row * p.q_row + head * p.q_head);
-        __syncthreads();
-        for (int d = lane; d < kDim; d += 64) qs[d] = (float)q[d];
-        __syncthreads();
-        float top = -INFINITY, sum = 0, acc[kDim / 64] = {};
-        for (int64_t j0 = start; j0 < stop; j0 += 64) {
-            const int64_t j = j0 + lane;
-            float s = -INFINITY;
-            int64_t page = -1;
-            if (j < stop) page = p.pages[seq * p.pages_stride + (j >> p.page_bits)];
-            const int64_t r = j & (((int64_t)1 << p.page_bits) - 1);
-            if (page >= 0 && page < p.num_pages) {
-                s = 0;
-                for (int d = 0; d < kDim; ++d)
-                    s += qs[d] * kept<T, kQuant>(p, p.k, p.k_scale, page, kv, r, d);
-                s *= p.scale;
-            } else {
-                page = -1;
-            }
-            float m = s;
-            for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-            const float next = fmaxf(top, m);
-            if (next == -INFINITY) continue;  // nothing seen yet: alike in every lane
-            const float keep = expf(top - next), w = page < 0 ? 0.0f : expf(s - next);
-            top = next;
-            __syncthreads();
-            ps[lane] = w;
-            at[lane] = page < 0 ? -1 : page << p.page_bits | r;
-            __syncthreads();
-            sum = sum * keep + w;
-            for (int i = 0; i < kDim / 64; ++i) {
-                acc[i] *= keep;
-                for (int t = 0; t < 64; ++t)
-                    if (at[t] >= 0)
-                        acc[i] += ps[t] * kept<T, kQuant>(p, p.v, p.v_scale, at[t] >> p.page_bits, kv,
-                                                          at[t] & (((int64_t)1 << p.page_bits) - 1),
-                                                          lane + 64 * i);
-            }
-        }
-        for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
-        T* out = reinterpret_cast<T*>(p.out + row * p.out_row + head * p.out_head);
-        for (int i = 0; i < kDim / 64; ++i) out[lane + 64 * i] = (T)(sum == 0 ? 0.0f : acc[i] / sum);
+        return v;
+    } else {
+        return __builtin_bit_cast(x8, l.w[f]);
     }
 }
 
+// Four keys of 16 positions each for 16 lanes: lane i addresses 4 positions of
+// key i / 4 and gets position i of the four keys.
+template <class T>
+__device__ inline typename Vec<T>::x4 read_transposed(const T* at) {
+    using Lds = __attribute__((address_space(3))) s16x4;
+    return __builtin_bit_cast(typename Vec<T>::x4,
+                              __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(void*)at));
+}
+
+// The largest of the four lanes that share lane mod 16, and their sum.
+__device__ inline float max4(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    x = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+    const uint32_t v = __builtin_bit_cast(uint32_t, x);
+    const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+__device__ inline float sum4(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+template <class T>
+__device__ inline bool not_finite(typename Vec<T>::x8 v) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bad |= !(fabsf((float)v[i]) <= 3.4e38f);
+    return bad;
+}
+
+// Where a sequence's queries and keys are.
+struct Seq {
+    int64_t first, len;  // its first row; keys
+    int32_t n;           // queries
+};
+__device__ inline Seq sequence(const Attend& p, int b) {
+    Seq s;
+    int64_t end = b + 1;
+    s.first = b;
+    if (p.q_start) {
+        s.first = p.q_start[b];
+        end = p.q_start[b + 1];
+    }
+    s.len = p.lengths[b];
+    // queries outside the rows are left out; the last row stays the last key's
+    if (end < s.first || end > p.rows || s.first < 0) end = s.first = 0;
+    s.n = (int32_t)(end - s.first);
+    return s;
+}
+
+// ---------------------------------------------------------------------------
+// Few queries a sequence: bound by reading the cache. A workgroup takes 16
+// (query, head of the group) rows of a sequence and cache head over a part of
+// its keys; its waves take steps of 32 keys in turn, each with its own running
+// maximum and sum, and load the next step's keys and values while they work on
+// one. Waves join in LDS, parts in `work` by the last workgroup to arrive.
+constexpr int kRowsHere = 16, kFewWaves = 4;
+
+template <int kDim>
+constexpr int part_floats() {
+    return kRowsHere * kDim + 2 * kRowsHere;  // sums, then maximum and total of each row
+}
+
+template <class T, bool kQuant, int kDim>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few(Attend p, int row_tiles, int parts_most,
+                                                             int part_keys, uint32_t* counters,
+                                                             float* partial) {
+    using x8 = typename Vec<T>::x8;
+    using x4 = typename Vec<T>::x4;
+    using Key = Loaded<T, kQuant, kDim>;
+    constexpr int kFrags = kDim / 32, kOut = kDim / 16;
+    constexpr int kRowBytes = kDim * 2 + 32;  // 16 keys' words of one position apart in banks
+    constexpr int kVs = kStep * kRowBytes / 2;
+    constexpr int kOutRow = kDim + 4;
+    __shared__ __attribute__((aligned(16))) T vs[kFewWaves * kVs];
+    __shared__ float tops[kFewWaves][kRowsHere], sums[kFewWaves][kRowsHere];
+    static_assert(kFewWaves * kVs * 2 >= kFewWaves * kRowsHere * kOutRow * 4 || kDim == 64);
+    __shared__ __attribute__((aligned(16))) float outs[kDim == 64 ? kFewWaves * kRowsHere * kOutRow : 4];
+    float* const red = kDim == 64 ? outs : reinterpret_cast<float*>(vs);
+
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
+    const int kv = blockIdx.y, b = blockIdx.z;
+    const int tile0 = blockIdx.x % row_tiles, my_part = blockIdx.x / row_tiles;
+    const Seq seq = sequence(p, b);
+    const int rows = seq.n * p.group;
+    const uint8_t* const kbase = p.k + kv * p.head_stride;
+    const uint8_t* const vbase = p.v + kv * p.head_stride;
+    const int32_t* const table = p.pages + b * p.pages_stride;
+
+    // rows past the tiles that the launch was shaped for: by one workgroup each
+    for (int tile = tile0; tile * kRowsHere < rows; tile += row_tiles) {
+        const bool extra = tile >= row_tiles;
+        if (extra && my_part) return;
+        // this lane's row: its query, head, and the keys it sees
+        const int r = tile * kRowsHere + row, t = r / p.group, g = r % p.group;
+        const bool live = r < rows;
+        const int64_t pos = seq.len - seq.n + t;
+        int64_t hi = live ? max((int64_t)0, min(pos + 1, p.capacity)) : 0;
+        int64_t lo = live && p.window ? max((int64_t)0, pos - p.window + 1) : 0;
+        // of all rows: the first and last query's are the ends
+        const int t_first = tile * kRowsHere / p.group;
+        const int t_last = min(rows - 1, tile * kRowsHere + kRowsHere - 1) / p.group;
+        const int64_t pos0 = seq.len - seq.n + t_first, pos1 = seq.len - seq.n + t_last;
+        const int64_t hi_all = max((int64_t)0, min(pos1 + 1, p.capacity));
+        const int64_t hi_min = max((int64_t)0, min(pos0 + 1, p.capacity));
+        const int64_t lo_all = p.window ? max((int64_t)0, pos0 - p.window + 1) : 0;
+        const int64_t lo_max = p.window ? max((int64_t)0, pos1 - p.window + 1) : 0;
+        const int64_t reach = max((int64_t)0, hi_all - lo_all);
+        int parts = (int)max((int64_t)1, min((int64_t)parts_most, (reach + part_keys - 1) / part_keys));
+        if (extra) parts = 1;
+        if (my_part >= parts) return;
+        const int64_t each = ((reach + parts - 1) / parts + kStep - 1) / kStep * kStep;
+        const int64_t begin = lo_all + my_part * each, end = min(hi_all, begin + each);
+
+        x8 q[kFrags];
+        const uint8_t* const qrow = p.q + (seq.first + min(t, seq.n - 1)) * p.q_row +
+                                    ((int64_t)kv * p.group + g) * p.q_head;
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+            q[f] = *reinterpret_cast<const x8*>(qrow + first_position<kQuant>(f, part) * 2);
+        const float scale = p.scale * 1.44269504f;
+
+        f32x4 o[kOut] = {};
+        float top = -INFINITY, sum = 0;
+        // keys 0 .. 15 and 16 .. 31 of a step: this lane's is `row` of each
+        struct Step {
+            Key k[2], v[2];
+            bool there[2];
+        };
+        auto load = [&](int64_t j0, Step& to) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t j = j0 + h * 16 + row;
+                int64_t page = -1;
+                if (j < end) page = table[j >> p.page_bits];
+                to.there[h] = page >= 0 && page < p.num_pages;
+                to.k[h] = Key{};
+                to.v[h] = Key{};
+                if (to.there[h]) {
+                    const int64_t in = j & (((int64_t)1 << p.page_bits) - 1);
+                    const int64_t at = page * p.page_stride + in * p.token_stride + part * 16;
+#pragma unroll
+                    for (int c = 0; c < Key::kWords; ++c) {
+                        to.k[h].w[c] = *reinterpret_cast<const u32x4*>(kbase + at + c * 64);
+                        to.v[h].w[c] = *reinterpret_cast<const u32x4*>(vbase + at + c * 64);
+                    }
+                    if (kQuant) {
+                        const int64_t sat = page * p.scale_page_stride + kv * p.scale_head_stride +
+                                            in * p.scale_token_stride;
+                        if (kDim == 128) {
+                            to.k[h].scale = *reinterpret_cast<const uint32_t*>(p.k_scale + sat);
+                            to.v[h].scale = *reinterpret_cast<const uint32_t*>(p.v_scale + sat);
+                        } else {
+                            to.k[h].scale = *reinterpret_cast<const uint16_t*>(p.k_scale + sat);
+                            to.v[h].scale = *reinterpret_cast<const uint16_t*>(p.v_scale + sat);
+                        }
+                    }
+                }
+            }
+        };
+        T* const mine = vs + wave * kVs;
+        auto work = [&](int64_t j0, const Step& in) {
+            f32x4 s[2] = {};
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[h] = mfma16(fragment(in.k[h], f, part), q[f], s[h]);
+            __builtin_amdgcn_sched_barrier(0);
+            bool odd = false;  // values that are not finite
+            const bool edge = j0 < lo_max || j0 + kStep > hi_min;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int f = 0; f < kFrags; ++f) {
+                    const x8 v = fragment(in.v[h], f, part);
+                    if (edge && not_finite<T>(v)) odd = true;
+                    *reinterpret_cast<x8*>(mine + (h * 16 + row) * (kRowBytes / 2) +
+                                           first_position<kQuant>(f, part)) = v;
+                }
+            __builtin_amdgcn_sched_barrier(0);
+            const uint64_t there0 = __ballot(in.there[0]), there1 = __ballot(in.there[1]);
+            const uint32_t there = (uint32_t)(there0 & 0xffff) | (uint32_t)(there1 & 0xffff) << 16;
+            const bool whole = there == 0xffffffffu && !edge;
+            float m = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[h][e] *= scale;
+                    if (!whole) {
+                        const int at = h * 16 + part * 4 + e;
+                        const int64_t j = j0 + at;
+                        if (!(there >> at & 1) || j < lo || j >= hi) s[h][e] = -INFINITY;
+                    }
+                    m = fmaxf(m, s[h][e]);
+                }
+            m = max4(m);
+            if (__any(m > top)) {
+                const float next = fmaxf(top, m), keep = next == -INFINITY ? 1.0f : exp2f(top - next);
+                top = next;
+                sum *= keep;
+#pragma unroll
+                for (int n = 0; n < kOut; ++n) o[n] *= keep;
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
+            x8 w;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[h][e] = __builtin_amdgcn_exp2f(s[h][e] - base);
+                    sum += s[h][e];
+                    w[h * 4 + e] = (T)s[h][e];
+                }
+            if (edge && __any(odd)) {
+                // zero such keys and add what those queries have of them that see them
+                const uint64_t b0 = __ballot(odd);
+                const uint32_t bad = (uint32_t)((b0 | b0 >> 16 | b0 >> 32 | b0 >> 48) & 0xffff);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        for (int from = 0; from < 4; ++from) {
+                            if (!(bad >> (from * 4 + e) & 1)) continue;
+                            T* const key = mine + (h * 16 + from * 4 + e) * (kRowBytes / 2);
+                            const float weight = __shfl((float)w[h * 4 + e], from * 16 + row);
+                            const int at = h * 16 + from * 4 + e;
+                            const bool seen = there >> at & 1 && j0 + at >= lo && j0 + at < hi;
+#pragma unroll
+                            for (int n = 0; n < kOut; ++n)
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) {
+                                    const float v = (float)key[n * 16 + part * 4 + x];
+                                    if (seen) o[n][x] += weight * v;
+                                }
+                            __builtin_amdgcn_wave_barrier();
+                            for (int d = lane; d < kDim; d += 64) key[d] = (T)0.0f;
+                        }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const T* const at = mine + (part * 4 + row / 4) * (kRowBytes / 2) + row % 4 * 4;
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) {
+                const x4 v0 = read_transposed<T>(at + n * 16);
+                const x4 v1 = read_transposed<T>(at + 16 * (kRowBytes / 2) + n * 16);
+                o[n] = mfma16(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), w, o[n]);
+            }
+        };
+        Step s0, s1;
+        constexpr int64_t kTurn = kFewWaves * kStep;
+        int64_t j0 = begin + wave * kStep;
+        if (j0 < end) load(j0, s0);
+        while (j0 < end) {
+            if (j0 + kTurn < end) load(j0 + kTurn, s1);
+            work(j0, s0);
+            j0 += kTurn;
+            if (j0 >= end) break;
+            if (j0 + kTurn < end) load(j0 + kTurn, s0);
+            work(j0, s1);
+            j0 += kTurn;
+        }
+
+        // join the waves
+        sum = sum4(sum);
+        if (part == 0) {
+            tops[wave][row] = top;
+            sums[wave][row] = sum;
+        }
+        __syncthreads();
+        float all_top = tops[0][row], all_sum = 0;
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) all_top = fmaxf(all_top, tops[w][row]);
+        const float base = all_top == -INFINITY ? 0.0f : all_top;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w)
+            all_sum += sums[w][row] * __builtin_amdgcn_exp2f(tops[w][row] - base);
+        const float keep = __builtin_amdgcn_exp2f(top - base);
+#pragma unroll
+        for (int n = 0; n < kOut; ++n)
+            *reinterpret_cast<f32x4*>(&red[(wave * kRowsHere + row) * kOutRow + n * 16 + part * 4]) =
+                o[n] * keep;
+        __syncthreads();
+        if (wave == 0 && part == 0) {
+            tops[0][row] = all_top;
+            sums[0][row] = all_sum;
+        }
+        __syncthreads();
+        // a thread's quads of the joined rows, in red[0]
+        constexpr int kQuads = kRowsHere * kDim / 4;
+        for (int e = threadIdx.x; e < kQuads; e += kFewWaves * 64) {
+            float* const at = &red[e / (kDim / 4) * kOutRow + e % (kDim / 4) * 4];
+            f32x4 v = *reinterpret_cast<f32x4*>(at);
+#pragma unroll
+            for (int w = 1; w < kFewWaves; ++w)
+                v += *reinterpret_cast<f32x4*>(at + w * kRowsHere * kOutRow);
+            *reinterpret_cast<f32x4*>(at) = v;
+        }
+        if (parts > 1) {
+            constexpr int kFloats = part_floats<kDim>();
+            const int64_t unit = ((int64_t)b * gridDim.y + kv) * row_tiles + tile;
+            const Rsrc all = buffer(partial + unit * parts_most * kFloats, (int64_t)parts * kFloats * 4);
+            const uint32_t here = my_part * kFloats * 4;
+            for (int e = threadIdx.x; e < kQuads; e += kFewWaves * 64)
+                leave_part(all, here + e * 16,
+                           *reinterpret_cast<f32x4*>(
+                               &red[e / (kDim / 4) * kOutRow + e % (kDim / 4) * 4]));
+            if (threadIdx.x < kRowsHere / 4) {
+                const int e = threadIdx.x * 4;
+                const f32x4 tp = {tops[0][e], tops[0][e + 1], tops[0][e + 2], tops[0][e + 3]};
+                const f32x4 sm = {sums[0][e], sums[0][e + 1], sums[0][e + 2], sums[0][e + 3]};
+                leave_part(all, here + (kQuads * 4 + e) * 4, tp);
+                leave_part(all, here + (kQuads * 4 + kRowsHere + e) * 4, sm);
+            }
+            if (!arrive_last(&counters[unit], parts)) continue;
+            for (int e = threadIdx.x; e < kQuads; e += kFewWaves * 64) {
+                const int rr = e / (kDim / 4), quad = rr / 4, in = rr % 4;
+                float best = -INFINITY;
+#pragma unroll 8
+                for (int y = 0; y < parts; ++y)
+                    best = fmaxf(best, take_part(all, (y * kFloats + kQuads * 4 + quad * 4) * 4)[in]);
+                const float from = best == -INFINITY ? 0.0f : best;
+                f32x4 v = {};
+                float total = 0;
+#pragma unroll 8
+                for (int y = 0; y < parts; ++y) {
+                    const uint32_t at = y * kFloats;
+                    const f32x4 o_y = take_part(all, (at + e * 4) * 4);
+                    const float m_y = take_part(all, (at + kQuads * 4 + quad * 4) * 4)[in];
+                    const float s_y = take_part(all, (at + kQuads * 4 + kRowsHere + quad * 4) * 4)[in];
+                    const float k_y = __builtin_amdgcn_exp2f(m_y - from);
+                    v += o_y * k_y;
+                    total += s_y * k_y;
+                }
+                *reinterpret_cast<f32x4*>(&red[rr * kOutRow + e % (kDim / 4) * 4]) = v;
+                if (e % (kDim / 4) == 0) sums[0][rr] = total;
+            }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < kQuads; e += kFewWaves * 64) {
+            const int rr = e / (kDim / 4), d = e % (kDim / 4) * 4, at = tile * kRowsHere + rr;
+            if (at >= rows) continue;
+            const float total = sums[0][rr], inverse = total == 0 ? 0.0f : 1.0f / total;
+            const f32x4 v = *reinterpret_cast<f32x4*>(&red[rr * kOutRow + d]) * inverse;
+            x4 y;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] = (T)(total == 0 ? 0.0f : v[x]);
+            *reinterpret_cast<x4*>(p.out + (seq.first + at / p.group) * p.out_row +
+                                   ((int64_t)kv * p.group + at % p.group) * p.out_head + d * 2) = y;
+        }
+        __syncthreads();
+    }
+}
+
+struct Work {
+    uint32_t* counters = nullptr;
+    float* partial = nullptr;
+    uint64_t floats = 0;
+};
+
+template <class T, bool kQuant, int kDim>
+void launch_dim(const Attend& p, int64_t max_q, int64_t max_len, const Work& work,
+                hipStream_t stream) {
+    const int kv_heads = p.heads / p.group;
+    const int64_t row_tiles = std::max<int64_t>(1, (std::max<int64_t>(max_q, 1) * p.group + 15) / 16);
+    const int64_t units = row_tiles * kv_heads * p.seqs;
+    int64_t reach = max_len > 0 ? std::min(max_len, p.capacity) : p.capacity;
+    if (p.window) reach = std::min<int64_t>(reach, p.window + max_q);
+    // parts of a sequence: enough workgroups for four a compute unit, of 256
+    // keys or more
+    int64_t part_keys = 256, parts = 1;
+    if (work.partial && units <= (int64_t)kWorkCounters) {
+        parts = std::min<int64_t>((reach + part_keys - 1) / part_keys,
+                                  std::max<int64_t>(1, 1024 / units));
+        parts = std::min<int64_t>(parts, work.floats / (units * part_floats<kDim>()));
+        parts = std::max<int64_t>(1, parts);
+        part_keys = std::max<int64_t>(part_keys, (reach + parts - 1) / parts);
+    }
+    attend_few<T, kQuant, kDim>
+        <<<dim3((uint32_t)(row_tiles * parts), kv_heads, p.seqs), kFewWaves * 64, 0, stream>>>(
+            p, (int)row_tiles, (int)parts, (int)std::min<int64_t>(part_keys, INT32_MAX / 2),
+            work.counters, work.partial);
+}
+
 template <class T, bool kQuant>
-void launch(const Attend& p, int dim, hipStream_t stream) {
-    const dim3 grid((uint32_t)std::min<int64_t>(p.rows, 1 << 20), p.heads);
+void launch(const Attend& p, int dim, int64_t max_q, int64_t max_len, const Work& work,
+            hipStream_t stream) {
     if (dim == 64)
-        attend_rows<T, kQuant, 64><<<grid, 64, 0, stream>>>(p);
+        launch_dim<T, kQuant, 64>(p, max_q, max_len, work, stream);
     else
-        attend_rows<T, kQuant, 128><<<grid, 64, 0, stream>>>(p);
+        launch_dim<T, kQuant, 128>(p, max_q, max_len, work, stream);
 }
 
 int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
@@ -178,10 +543,19 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
     p.group = a.heads / c.heads;
     p.page_bits = __builtin_ctz(c.page);
     p.scale = a.scale;
+    Work work;
+    if (a.work_bytes > kWorkHead) {
+        work.counters = static_cast<uint32_t*>(a.work);
+        work.partial = reinterpret_cast<float*>(static_cast<char*>(a.work) + kWorkHead);
+        work.floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
+    }
+    const int64_t max_q = a.q_start ? a.max_q : 1;
     if (a.dtype == II_BF16)
-        quant ? launch<__bf16, true>(p, c.dim, stream) : launch<__bf16, false>(p, c.dim, stream);
+        quant ? launch<__bf16, true>(p, c.dim, max_q, a.max_len, work, stream)
+              : launch<__bf16, false>(p, c.dim, max_q, a.max_len, work, stream);
     else
-        quant ? launch<_Float16, true>(p, c.dim, stream) : launch<_Float16, false>(p, c.dim, stream);
+        quant ? launch<_Float16, true>(p, c.dim, max_q, a.max_len, work, stream)
+              : launch<_Float16, false>(p, c.dim, max_q, a.max_len, work, stream);
     return launched(fn);
 }
 

@@ -594,7 +594,7 @@ __global__ __launch_bounds__(kTileWaves * 64, kM * kN == 256 * 256 ? 2 : 4) void
             begin_tile();
         }
         bool mine = true;
-        if (gridDim.y > 1) {
+        if (kM * kN < 256 * 256 && gridDim.y > 1) {
             constexpr int64_t kSums = (int64_t)kM * kN;
             const Rsrc parts = buffer(partial + (int64_t)done * gridDim.y * kSums,
                                       (int64_t)gridDim.y * kSums * 4);
