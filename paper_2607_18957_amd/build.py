@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libii.so")
 SOURCES = ["plan.cpp", "scatter.hip", "runtime.hip", "ops.cpp", "linear.hip", "cache.hip",
-           "attend.hip"]
+           "attend.hip", "attend_many.hip"]
 ARCH = os.environ.get("II_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [

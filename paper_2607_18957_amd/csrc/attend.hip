@@ -1,34 +1,17 @@
 // ii_attend: attention of new tokens over a paged key/value cache.
 #include <algorithm>
-#include <cmath>
 
-#include "ops.h"
-#include "ops_device.h"
+#include "attend.h"
 
 namespace ii {
 namespace {
 
-struct Attend {
-    const uint8_t *q, *k, *v, *k_scale, *v_scale;
-    uint8_t* out;
-    int64_t q_row, q_head, out_row, out_head;  // strides, bytes
-    int64_t page_stride, head_stride, token_stride;
-    int64_t scale_page_stride, scale_head_stride, scale_token_stride;
-    const int32_t *pages, *lengths, *q_start;
-    int64_t pages_stride, capacity;  // capacity: keys a table's columns hold
-    int64_t rows, window, num_pages;
-    int32_t seqs, heads, group, page_bits;
-    float scale;
-};
-
-// ---------------------------------------------------------------------------
-// What the kernels share. Scores are formed transposed, keys by queries
-// (S^T = K Q^T), and so is the result (O^T = V^T P^T): with 16 x 16 x 32
-// products a lane then holds, of one query (its lane mod 16), the scores of
-// keys 4 (lane / 16) + r of each 16, which are just the operand that the second
-// product takes, if the 32 keys of a step are numbered 4 by 4: no score
-// crosses lanes. V^T comes out of LDS by the transposing read, whose 16 lanes
-// give 4 keys each of 16 positions.
+// Scores are formed transposed, keys by queries (S^T = K Q^T), and so is the
+// result (O^T = V^T P^T): with 16 x 16 x 32 products a lane then holds, of one
+// query (its lane mod 16), the scores of keys 4 (lane / 16) + r of each 16,
+// which are just the operand that the second product takes, if the 32 keys of
+// a step are numbered 4 by 4: no score crosses lanes. V^T comes out of LDS by
+// the transposing read, whose 16 lanes give 4 keys each of 16 positions.
 
 constexpr int kStep = 32;  // keys a wave takes at once
 
@@ -47,14 +30,6 @@ struct Loaded {
 template <bool kQuant>
 __device__ inline int first_position(int f, int part) {
     return kQuant ? f / 2 * 64 + part * 16 + f % 2 * 8 : f * 32 + part * 8;
-}
-__device__ inline bf16x2 unpack(uint32_t codes, float scale, bf16x2, bool high) {
-    return high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true)
-                : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
-}
-__device__ inline f16x2 unpack(uint32_t codes, float scale, f16x2, bool high) {
-    return high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, true)
-                : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, false);
 }
 template <class T, bool kQuant, int kDim>
 __device__ inline typename Vec<T>::x8 fragment(const Loaded<T, kQuant, kDim>& l, int f, int part) {
@@ -79,15 +54,6 @@ __device__ inline typename Vec<T>::x8 fragment(const Loaded<T, kQuant, kDim>& l,
     }
 }
 
-// Four keys of 16 positions each for 16 lanes: lane i addresses 4 positions of
-// key i / 4 and gets position i of the four keys.
-template <class T>
-__device__ inline typename Vec<T>::x4 read_transposed(const T* at) {
-    using Lds = __attribute__((address_space(3))) s16x4;
-    return __builtin_bit_cast(typename Vec<T>::x4,
-                              __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(void*)at));
-}
-
 // The largest of the four lanes that share lane mod 16, and their sum.
 __device__ inline float max4(float x) {
     const uint32_t u = __builtin_bit_cast(uint32_t, x);
@@ -102,34 +68,6 @@ __device__ inline float sum4(float x) {
     return x + __shfl_xor(x, 32);
 }
 
-template <class T>
-__device__ inline bool not_finite(typename Vec<T>::x8 v) {
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) bad |= !(fabsf((float)v[i]) <= 3.4e38f);
-    return bad;
-}
-
-// Where a sequence's queries and keys are.
-struct Seq {
-    int64_t first, len;  // its first row; keys
-    int32_t n;           // queries
-};
-__device__ inline Seq sequence(const Attend& p, int b) {
-    Seq s;
-    int64_t end = b + 1;
-    s.first = b;
-    if (p.q_start) {
-        s.first = p.q_start[b];
-        end = p.q_start[b + 1];
-    }
-    s.len = p.lengths[b];
-    // queries outside the rows are left out; the last row stays the last key's
-    if (end < s.first || end > p.rows || s.first < 0) end = s.first = 0;
-    s.n = (int32_t)(end - s.first);
-    return s;
-}
-
 // ---------------------------------------------------------------------------
 // Few queries a sequence: bound by reading the cache. A workgroup takes 16
 // (query, head of the group) rows of a sequence and cache head over a part of
@@ -138,15 +76,18 @@ __device__ inline Seq sequence(const Attend& p, int b) {
 // one. Waves join in LDS, parts in `work` by the last workgroup to arrive.
 constexpr int kRowsHere = 16, kFewWaves = 4;
 
+// The most rows of a sequence that are few.
+constexpr int kFewRows = 64;
+
 template <int kDim>
 constexpr int part_floats() {
     return kRowsHere * kDim + 2 * kRowsHere;  // sums, then maximum and total of each row
 }
 
 template <class T, bool kQuant, int kDim>
-__global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few(Attend p, int row_tiles, int parts_most,
-                                                             int part_keys, uint32_t* counters,
-                                                             float* partial) {
+__global__ __launch_bounds__(kFewWaves * 64, 2) void attend_split(Attend p, int row_tiles, int parts_most,
+                                                             int part_keys, int most_rows,
+                                                             uint32_t* counters, float* partial) {
     using x8 = typename Vec<T>::x8;
     using x4 = typename Vec<T>::x4;
     using Key = Loaded<T, kQuant, kDim>;
@@ -165,6 +106,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few(Attend p, int ro
     const int tile0 = blockIdx.x % row_tiles, my_part = blockIdx.x / row_tiles;
     const Seq seq = sequence(p, b);
     const int rows = seq.n * p.group;
+    if (rows > most_rows) return;
     const uint8_t* const kbase = p.k + kv * p.head_stride;
     const uint8_t* const vbase = p.v + kv * p.head_stride;
     const int32_t* const table = p.pages + b * p.pages_stride;
@@ -179,20 +121,15 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few(Attend p, int ro
         const int64_t pos = seq.len - seq.n + t;
         int64_t hi = live ? max((int64_t)0, min(pos + 1, p.capacity)) : 0;
         int64_t lo = live && p.window ? max((int64_t)0, pos - p.window + 1) : 0;
-        // of all rows: the first and last query's are the ends
-        const int t_first = tile * kRowsHere / p.group;
-        const int t_last = min(rows - 1, tile * kRowsHere + kRowsHere - 1) / p.group;
-        const int64_t pos0 = seq.len - seq.n + t_first, pos1 = seq.len - seq.n + t_last;
-        const int64_t hi_all = max((int64_t)0, min(pos1 + 1, p.capacity));
-        const int64_t hi_min = max((int64_t)0, min(pos0 + 1, p.capacity));
-        const int64_t lo_all = p.window ? max((int64_t)0, pos0 - p.window + 1) : 0;
-        const int64_t lo_max = p.window ? max((int64_t)0, pos1 - p.window + 1) : 0;
-        const int64_t reach = max((int64_t)0, hi_all - lo_all);
-        int parts = (int)max((int64_t)1, min((int64_t)parts_most, (reach + part_keys - 1) / part_keys));
+        const Reach all = reach_of(p, seq, tile * kRowsHere / p.group,
+                                   min(rows - 1, tile * kRowsHere + kRowsHere - 1) / p.group);
+        const int64_t hi_min = all.hi_min, lo_max = all.lo_max;
+        const int64_t reach = max((int64_t)0, all.hi - all.lo);
+        int parts = parts_of(all, parts_most, part_keys);
         if (extra) parts = 1;
         if (my_part >= parts) return;
         const int64_t each = ((reach + parts - 1) / parts + kStep - 1) / kStep * kStep;
-        const int64_t begin = lo_all + my_part * each, end = min(hi_all, begin + each);
+        const int64_t begin = all.lo + my_part * each, end = min(all.hi, begin + each);
 
         x8 q[kFrags];
         const uint8_t* const qrow = p.q + (seq.first + min(t, seq.n - 1)) * p.q_row +
@@ -380,18 +317,18 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few(Attend p, int ro
         if (parts > 1) {
             constexpr int kFloats = part_floats<kDim>();
             const int64_t unit = ((int64_t)b * gridDim.y + kv) * row_tiles + tile;
-            const Rsrc all = buffer(partial + unit * parts_most * kFloats, (int64_t)parts * kFloats * 4);
+            const Rsrc left = buffer(partial + unit * parts_most * kFloats, (int64_t)parts * kFloats * 4);
             const uint32_t here = my_part * kFloats * 4;
             for (int e = threadIdx.x; e < kQuads; e += kFewWaves * 64)
-                leave_part(all, here + e * 16,
+                leave_part(left, here + e * 16,
                            *reinterpret_cast<f32x4*>(
                                &red[e / (kDim / 4) * kOutRow + e % (kDim / 4) * 4]));
             if (threadIdx.x < kRowsHere / 4) {
                 const int e = threadIdx.x * 4;
                 const f32x4 tp = {tops[0][e], tops[0][e + 1], tops[0][e + 2], tops[0][e + 3]};
                 const f32x4 sm = {sums[0][e], sums[0][e + 1], sums[0][e + 2], sums[0][e + 3]};
-                leave_part(all, here + (kQuads * 4 + e) * 4, tp);
-                leave_part(all, here + (kQuads * 4 + kRowsHere + e) * 4, sm);
+                leave_part(left, here + (kQuads * 4 + e) * 4, tp);
+                leave_part(left, here + (kQuads * 4 + kRowsHere + e) * 4, sm);
             }
             if (!arrive_last(&counters[unit], parts)) continue;
             for (int e = threadIdx.x; e < kQuads; e += kFewWaves * 64) {
@@ -399,16 +336,16 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few(Attend p, int ro
                 float best = -INFINITY;
 #pragma unroll 8
                 for (int y = 0; y < parts; ++y)
-                    best = fmaxf(best, take_part(all, (y * kFloats + kQuads * 4 + quad * 4) * 4)[in]);
+                    best = fmaxf(best, take_part(left, (y * kFloats + kQuads * 4 + quad * 4) * 4)[in]);
                 const float from = best == -INFINITY ? 0.0f : best;
                 f32x4 v = {};
                 float total = 0;
 #pragma unroll 8
                 for (int y = 0; y < parts; ++y) {
                     const uint32_t at = y * kFloats;
-                    const f32x4 o_y = take_part(all, (at + e * 4) * 4);
-                    const float m_y = take_part(all, (at + kQuads * 4 + quad * 4) * 4)[in];
-                    const float s_y = take_part(all, (at + kQuads * 4 + kRowsHere + quad * 4) * 4)[in];
+                    const f32x4 o_y = take_part(left, (at + e * 4) * 4);
+                    const float m_y = take_part(left, (at + kQuads * 4 + quad * 4) * 4)[in];
+                    const float s_y = take_part(left, (at + kQuads * 4 + kRowsHere + quad * 4) * 4)[in];
                     const float k_y = __builtin_amdgcn_exp2f(m_y - from);
                     v += o_y * k_y;
                     total += s_y * k_y;
@@ -433,20 +370,12 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few(Attend p, int ro
     }
 }
 
-struct Work {
-    uint32_t* counters = nullptr;
-    float* partial = nullptr;
-    uint64_t floats = 0;
-};
-
 template <class T, bool kQuant, int kDim>
-void launch_dim(const Attend& p, int64_t max_q, int64_t max_len, const Work& work,
-                hipStream_t stream) {
+void launch_dim(const Attend& p, int64_t max_q, int64_t reach, int most_rows,
+                const AttendWork& work, hipStream_t stream) {
     const int kv_heads = p.heads / p.group;
-    const int64_t row_tiles = std::max<int64_t>(1, (std::max<int64_t>(max_q, 1) * p.group + 15) / 16);
+    const int64_t row_tiles = (max_q * p.group + kRowsHere - 1) / kRowsHere;
     const int64_t units = row_tiles * kv_heads * p.seqs;
-    int64_t reach = max_len > 0 ? std::min(max_len, p.capacity) : p.capacity;
-    if (p.window) reach = std::min<int64_t>(reach, p.window + max_q);
     // parts of a sequence: enough workgroups for four a compute unit, of 256
     // keys or more
     int64_t part_keys = 256, parts = 1;
@@ -457,19 +386,26 @@ void launch_dim(const Attend& p, int64_t max_q, int64_t max_len, const Work& wor
         parts = std::max<int64_t>(1, parts);
         part_keys = std::max<int64_t>(part_keys, (reach + parts - 1) / parts);
     }
-    attend_few<T, kQuant, kDim>
+    attend_split<T, kQuant, kDim>
         <<<dim3((uint32_t)(row_tiles * parts), kv_heads, p.seqs), kFewWaves * 64, 0, stream>>>(
             p, (int)row_tiles, (int)parts, (int)std::min<int64_t>(part_keys, INT32_MAX / 2),
-            work.counters, work.partial);
+            most_rows, work.counters, work.partial);
 }
 
-template <class T, bool kQuant>
-void launch(const Attend& p, int dim, int64_t max_q, int64_t max_len, const Work& work,
-            hipStream_t stream) {
-    if (dim == 64)
-        launch_dim<T, kQuant, 64>(p, max_q, max_len, work, stream);
-    else
-        launch_dim<T, kQuant, 128>(p, max_q, max_len, work, stream);
+// Attention of the sequences with up to most_rows (query, head of a group)
+// rows.
+void attend_few(const Attend& p, int dtype, bool quant, int dim, int64_t max_q, int64_t reach,
+                int most_rows, const AttendWork& work, hipStream_t stream) {
+    const auto with = [&](auto t, auto q) {
+        using T = decltype(t);
+        constexpr bool kQuant = decltype(q)::value;
+        dim == 64 ? launch_dim<T, kQuant, 64>(p, max_q, reach, most_rows, work, stream)
+                  : launch_dim<T, kQuant, 128>(p, max_q, reach, most_rows, work, stream);
+    };
+    const auto type = [&](auto q) {
+        dtype == II_BF16 ? with(__bf16{}, q) : with(_Float16{}, q);
+    };
+    quant ? type(std::true_type{}) : type(std::false_type{});
 }
 
 int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
@@ -485,7 +421,7 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
     if (a.heads < 1 || a.heads % c.heads || a.heads > 65535)
         return fail(II_EINVAL, "%s: %d query heads over %d cache heads", fn, a.heads, c.heads);
     if (a.rows < 0 || a.rows > INT32_MAX || a.seqs < 0 || a.seqs > 65535 || a.max_q < 0 ||
-        a.max_len < 0 || a.window < 0)
+        a.max_len < 0 || a.window < 0 || a.rows * a.heads > INT32_MAX / 2)
         return fail(II_EINVAL, "%s: a size is out of range", fn);
     if (a.columns < 0 || a.columns > ((int64_t)1 << 40) / c.page || a.pages_stride < 0)
         return fail(II_EINVAL, "%s: a page table of %lld columns, stride %lld", fn,
@@ -543,19 +479,24 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
     p.group = a.heads / c.heads;
     p.page_bits = __builtin_ctz(c.page);
     p.scale = a.scale;
-    Work work;
+    AttendWork work;
     if (a.work_bytes > kWorkHead) {
         work.counters = static_cast<uint32_t*>(a.work);
         work.partial = reinterpret_cast<float*>(static_cast<char*>(a.work) + kWorkHead);
         work.floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
     }
-    const int64_t max_q = a.q_start ? a.max_q : 1;
-    if (a.dtype == II_BF16)
-        quant ? launch<__bf16, true>(p, c.dim, max_q, a.max_len, work, stream)
-              : launch<__bf16, false>(p, c.dim, max_q, a.max_len, work, stream);
-    else
-        quant ? launch<_Float16, true>(p, c.dim, max_q, a.max_len, work, stream)
-              : launch<_Float16, false>(p, c.dim, max_q, a.max_len, work, stream);
+    const int64_t max_q = a.q_start ? std::max<int64_t>(1, std::min(a.max_q, a.rows)) : 1;
+    const int64_t reach_q = a.max_len > 0 ? std::min(a.max_len, p.capacity) : p.capacity;
+    const int64_t reach = p.window ? std::min(reach_q, p.window + max_q) : reach_q;
+    // Sequences of many rows go to one kernel, the others to another. The call
+    // does not read the sizes, so both are launched unless all sequences have
+    // max_q queries.
+    const bool many = max_q * p.group > kFewRows, mixed = a.rows < a.seqs * max_q;
+    if (many)
+        attend_many(p, a.dtype, quant, c.dim, max_q, reach, mixed ? kFewRows : 0, work, stream);
+    if (!many || mixed)
+        attend_few(p, a.dtype, quant, c.dim, many ? std::max(1, kFewRows / p.group) : max_q, reach,
+                   many ? kFewRows : INT32_MAX, work, stream);
     return launched(fn);
 }
 
