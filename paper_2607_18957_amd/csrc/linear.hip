@@ -755,7 +755,8 @@ void launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
     // rows of x that the waves' own loads find in the caches: 1 x 4096 x 14336
     // 25.0 us against 28.1 through LDS, 1 x 128256 x 4096 177 against 186; from
     // 8 tokens on it is 29.2 against 27.4, 212 against 191
-    if (wide && p.m <= 4) return stream_waves<T, kGated, kGated ? 2 : 1, 1, 4>(p, work, stream);
+    // (its grid has a workgroup for each 16 rows; a dispatch counts 2^32 lanes)
+    if (wide && p.m <= 4 && p.n <= 1 << 26) return stream_waves<T, kGated, kGated ? 2 : 1, 1, 4>(p, work, stream);
     // rows that waves share through LDS, where it takes all waves of the card
     // to keep up with the memory and a tile's rows would be too few: 24 x 4096
     // x 14336 31.4 us against 33.6 in tiles; 24 x 14336 x 4096 with a gate
@@ -764,8 +765,8 @@ void launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
         if (p.m <= 16) return shared_launch<T, kGated, 1>(p, work, stream);
         return shared_launch<T, kGated, 2>(p, work, stream);
     }
-    // a tile's rows are addressed in 32 bits
-    const bool near = std::max({p.x_stride, p.w_stride, p.w2_stride}) < (1 << 21);
+    // a tile's rows are addressed in 32 bits (strides may be less than k)
+    const bool near = std::max({p.x_stride, p.w_stride, p.w2_stride, (int64_t)p.k}) < (1 << 21);
     const Choice c = choose_tile(p.m, p.n, p.k, kGated, work, wide && near ? 3 : 2);
     if (!wide || !near)
         return c.shape ? tile_launch<T, kGated, 128, 256, 2, false>(p, work, c.split, stream)
@@ -833,6 +834,7 @@ int check(const ii_linear_args& a) {
                     (long long)a.out_stride, (long long)a.n);
     if (!a.m || !a.n) return II_OK;
     const uint64_t m = a.m, n = a.n, k = a.k, size = 2, osize = a.out_dtype == II_F32 ? 4 : 2;
+    static const char* const kResidual = "residual";
     Rows out, r;
     int rc = check_rows(fn, "out", a.out, m, n * osize, (m > 1 ? a.out_stride : 0) * osize, osize,
                         &out);
@@ -847,7 +849,7 @@ int check(const ii_linear_args& a) {
                {"w2", a.w2, n, k, (uint64_t)a.w2_stride, false},
                {"bias", a.bias, 1, n, 0, false},
                {"bias2", a.bias2, 1, n, 0, false},
-               {"residual", a.residual, m, n, (uint64_t)a.residual_stride, false}};
+               {kResidual, a.residual, m, n, (uint64_t)a.residual_stride, false}};
     for (const auto& in : ins) {
         if (!in.p && !in.need) continue;
         uint64_t stride;
@@ -855,8 +857,8 @@ int check(const ii_linear_args& a) {
             return fail(II_EOVERFLOW, "%s: the stride of %s", fn, in.what);
         rc = check_rows(fn, in.what, in.p, in.rows, in.width * size, stride, size, &r);
         if (rc) return rc;
-        if (in.p == a.residual && in.p == a.out && a.out_dtype == a.dtype &&
-            (m == 1 || a.residual_stride == a.out_stride) && in.rows == m && in.width == n)
+        if (in.what == kResidual && in.p == a.out && a.out_dtype == a.dtype &&
+            (m == 1 || a.residual_stride == a.out_stride))
             continue;  // each element is read by the lane that then writes it
         rc = check_apart(fn, in.what, out, r);
         if (rc) return rc;

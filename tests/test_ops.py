@@ -566,3 +566,48 @@ def test_refusals(work):
     wide = torch.as_strided(cache.k, (4, 2, 16, 64), (2048, 512, 64, 1))
     refused("II_EINVAL", lambda: ops.ii_cache_write(
         ops.Cache(wide, wide, cache.k_scale, cache.v_scale), k, k, slots))
+
+
+def test_refusal_of_x_as_residual_and_out():
+    """out may be the residual, but not x or w too, though their shapes agree."""
+    a = torch.zeros(64, 64, dtype=BF16, device=DEV)
+    w = _normal(_gen(0), 64, 64)
+    for args in ((a, a, w), (a, w, a)):
+        with pytest.raises(ii.IIError) as e:
+            ops.ii_linear(*args, residual=a)
+        assert e.value.name == "II_EOVERLAP"
+    ops.ii_linear(a, w, w, residual=a)
+
+
+@pytest.mark.parametrize("m", [5, 40])
+def test_linear_long_rows_at_stride_0(m, work):
+    """Rows that broadcast, k past what 32-bit offsets of a tile reach: exact sums."""
+    k = (1 << 21) + 64
+    x = torch.ones(1, k, dtype=BF16, device=DEV)
+    x[0, ::2] = -1
+    x[0, -3:] = 2
+    out = torch.empty(m, 3, dtype=F32, device=DEV)
+    ops.ii_linear(out, x.expand(m, k), torch.ones(1, k, dtype=BF16, device=DEV).expand(3, k), work=work)
+    assert bool((out == x.double().sum().item()).all())
+
+
+def test_attend_a_few_queries_of_long_contexts(work):
+    """Some hundred rows over long contexts, split over keys and joined; decoding
+    requests beside them."""
+    for keys, queries in (([9000], [40]), ([20000, 7000], [33, 90]), ([12000, 5, 300, 0], [70, 1, 2, 1])):
+        b = _batch(_gen(len(keys)), keys, queries, 16, 4, 128, 64)
+        for w in (work, None, work[:3 << 20]):
+            _attend(*b, work=w, max_len=max(keys))
+        _attend(*b, work=work, window=3000)
+
+
+def test_attend_many_queries_of_extreme_scores(work):
+    """Maxima that grow by little and by much, a falling and a rising row."""
+    cache, q, tables, keys, starts = _batch(_gen(3), [600], [300], 8, 2, 128, 16, BF16, BF16)
+    ramp = torch.linspace(-4, 4, 600, device=DEV).to(BF16)
+    for j in range(600):
+        cache.k[tables[0][j // 16], :, j % 16] = ramp[j]
+    for by in (0.02, 0.1, -0.1, 3.0):
+        q.fill_(by)
+        _attend(cache, q, tables, keys, starts, work=work, scale=1.0)
+        _attend(cache, q, tables, keys, starts, work=work, scale=-1.0, window=77)
