@@ -73,13 +73,14 @@ __device__ inline float sum4(float x) {
 // (query, head of the group) rows of a sequence and cache head over a part of
 // its keys; its waves take steps of 32 keys in turn, each with its own running
 // maximum and sum, and load the next step's keys and values while they work on
-// one. 48 sequences of up to 8192 keys, 8 heads, 8 bits: 145 us; 2 of up to
-// 131072 in bf16: 244 us, 3.6 TB/s (with two sets of registers, which spilled,
-// 519). Waves join in LDS, parts in `work` by the last workgroup to arrive.
+// one. 48 sequences of up to 8192 keys, 8 heads, 8 bits: 113 us, 3.6 TB/s; 2 of
+// up to 131072 in bf16: 183 us, 4.7 TB/s. Waves join in LDS, parts in `work` by the last workgroup to arrive.
 constexpr int kRowsHere = 16, kFewWaves = 4;
 
 // The most rows of a sequence that are few.
 constexpr int kFewRows = 64;
+
+constexpr int kPartsMost = 96;
 
 template <int kDim>
 constexpr int part_floats() {
@@ -105,7 +106,11 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_split(Attend p, int 
 
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
     const int kv = blockIdx.y, b = blockIdx.z;
-    const int tile0 = blockIdx.x % row_tiles, my_part = blockIdx.x / row_tiles;
+    // Workgroups go to the 8 XCDs in turn. Short sequences have the first parts
+    // alone, so parts are numbered from another place in each sequence and head:
+    // with 8 parts the first would all be on one XCD.
+    const int tile0 = blockIdx.x % row_tiles;
+    const int my_part = (blockIdx.x / row_tiles + kv + b) % parts_most;
     const Seq seq = sequence(p, b);
     const int rows = seq.n * p.group;
     if (rows > most_rows) return;
@@ -341,27 +346,55 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_split(Attend p, int 
                 leave_part(left, here + (kQuads * 4 + kRowsHere + e) * 4, sm);
             }
             if (!arrive_last(&counters[unit], parts)) continue;
-            for (int e = threadIdx.x; e < kQuads; e += kFewWaves * 64) {
-                const int rr = e / (kDim / 4), quad = rr / 4, in = rr % 4;
-                float best = -INFINITY;
+            // maxima and totals first, all at once, then the sums, many parts'
+            // loads under way together: each waits for memory some us
+            float* const fade = red + kRowsHere * kOutRow;  // [part][row]: maxima, then factors
+            float* const totals = fade + kPartsMost * kRowsHere;
+            static_assert(2 * kPartsMost <= (kFewWaves - 1) * kOutRow);
+            for (int i = threadIdx.x; i < parts * 4; i += kFewWaves * 64) {
+                const uint32_t at = (i / 4 * kFloats + kQuads * 4 + i % 4 * 4) * 4;
+                *reinterpret_cast<f32x4*>(&fade[i * 4]) = take_part(left, at);
+                *reinterpret_cast<f32x4*>(&totals[i * 4]) = take_part(left, at + kRowsHere * 4);
+            }
+            __syncthreads();
+            constexpr int kStride = kFewWaves * 4;
+            float best = -INFINITY, total = 0;
+            for (int y = wave * 4 + part; y < parts; y += kStride)
+                best = fmaxf(best, fade[y * kRowsHere + row]);
+            best = max4(best);
+            if (part == 0) tops[wave][row] = best;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) best = fmaxf(best, tops[w][row]);
+            const float from = best == -INFINITY ? 0.0f : best;
+            for (int y = wave * 4 + part; y < parts; y += kStride) {
+                float& f = fade[y * kRowsHere + row];
+                f = __builtin_amdgcn_exp2f(f - from);
+                total += f * totals[y * kRowsHere + row];
+            }
+            total = sum4(total);
+            __syncthreads();
+            if (part == 0) sums[wave][row] = total;
+            constexpr int kMine = kQuads / (kFewWaves * 64);
+            f32x4 v[kMine] = {};
 #pragma unroll 8
-                for (int y = 0; y < parts; ++y)
-                    best = fmaxf(best, take_part(left, (y * kFloats + kQuads * 4 + quad * 4) * 4)[in]);
-                const float from = best == -INFINITY ? 0.0f : best;
-                f32x4 v = {};
-                float total = 0;
-#pragma unroll 8
-                for (int y = 0; y < parts; ++y) {
-                    const uint32_t at = y * kFloats;
-                    const f32x4 o_y = take_part(left, (at + e * 4) * 4);
-                    const float m_y = take_part(left, (at + kQuads * 4 + quad * 4) * 4)[in];
-                    const float s_y = take_part(left, (at + kQuads * 4 + kRowsHere + quad * 4) * 4)[in];
-                    const float k_y = __builtin_amdgcn_exp2f(m_y - from);
-                    v += o_y * k_y;
-                    total += s_y * k_y;
+            for (int y = 0; y < parts; ++y)
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) {
+                    const int e = threadIdx.x + i * kFewWaves * 64;
+                    v[i] += take_part(left, (y * kFloats + e * 4) * 4) *
+                            fade[y * kRowsHere + e / (kDim / 4)];
                 }
-                *reinterpret_cast<f32x4*>(&red[rr * kOutRow + e % (kDim / 4) * 4]) = v;
-                if (e % (kDim / 4) == 0) sums[0][rr] = total;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int e = threadIdx.x + i * kFewWaves * 64;
+                *reinterpret_cast<f32x4*>(&red[e / (kDim / 4) * kOutRow + e % (kDim / 4) * 4]) = v[i];
+            }
+            __syncthreads();
+            if (wave == 0 && part == 0) {
+#pragma unroll
+                for (int w = 1; w < kFewWaves; ++w) total += sums[w][row];
+                sums[0][row] = total;
             }
         }
         __syncthreads();
@@ -386,13 +419,18 @@ void launch_dim(const Attend& p, int64_t max_q, int64_t reach, int most_rows,
     const int kv_heads = p.heads / p.group;
     const int64_t row_tiles = (max_q * p.group + kRowsHere - 1) / kRowsHere;
     const int64_t units = row_tiles * kv_heads * p.seqs;
-    // parts of a sequence: enough workgroups for four a compute unit, of 256
-    // keys or more
-    int64_t part_keys = 256, parts = 1;
+    // Parts of a sequence, of 512 keys or more. The card holds 512 workgroups:
+    // few units take as many, so that none comes second; ragged ones in large
+    // numbers three times as many, so that long ones do not come last. Measured
+    // with 512, 1024, 1536, 2048: 16 units of up to 131072 keys 184, 204, 210,
+    // 208 us; 64 of up to 20001 58, 63, 58, 81; 256 of up to 8001 83, 78, 69, 73;
+    // 384 of up to 8192 165, 144, 113, 121. Parts of 256 keys: 1 x 4001 20 us
+    // against 18.
+    int64_t part_keys = 512, parts = 1;
     if (work.partial && units <= (int64_t)kWorkCounters) {
-        parts = std::min<int64_t>((reach + part_keys - 1) / part_keys,
-                                  std::max<int64_t>(1, 1024 / units));
-        parts = std::min<int64_t>(parts, work.floats / (units * part_floats<kDim>()));
+        parts = std::min<int64_t>({(reach + part_keys - 1) / part_keys,
+                                   (units <= 128 ? 512 : 1536) / units, kPartsMost,
+                                   (int64_t)(work.floats / (units * part_floats<kDim>()))});
         parts = std::max<int64_t>(1, parts);
         part_keys = std::max<int64_t>(part_keys, (reach + parts - 1) / parts);
     }
