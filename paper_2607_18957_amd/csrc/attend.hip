@@ -73,8 +73,8 @@ __device__ inline float sum4(float x) {
 // (query, head of the group) rows of a sequence and cache head over a part of
 // its keys; its waves take steps of 32 keys in turn, each with its own running
 // maximum and sum, and load the next step's keys and values while they work on
-// one. 48 sequences of up to 8192 keys, 8 heads, 8 bits: 113 us, 3.6 TB/s; 2 of
-// up to 131072 in bf16: 183 us, 4.7 TB/s. Waves join in LDS, parts in `work` by the last workgroup to arrive.
+// one. 48 sequences of up to 8192 keys, 8 heads, 8 bits: 94 us, 4.4 TB/s; 2 of
+// up to 131072 in bf16: 176 us, 4.9 TB/s. Waves join in LDS, parts in `work` by the last workgroup to arrive.
 constexpr int kRowsHere = 16, kFewWaves = 4;
 
 // The most rows of a sequence that are few.
@@ -104,7 +104,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_split(Attend p, int 
     __shared__ __attribute__((aligned(16))) float outs[kDim == 64 ? kFewWaves * kRowsHere * kOutRow : 4];
     float* const red = kDim == 64 ? outs : reinterpret_cast<float*>(vs);
 
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
+    const int lane = threadIdx.x % 64, row = lane % 16, part = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int kv = blockIdx.y, b = blockIdx.z;
     // Workgroups go to the 8 XCDs in turn. Short sequences have the first parts
     // alone, so parts are numbered from another place in each sequence and head:
@@ -153,7 +154,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_split(Attend p, int 
         // values as soon as these are in LDS, its pages a step before: one set
         // of registers, so that none of them spills, which would wait for it
         Key k[2], v[2];
-        int64_t page[2], at[2], sat[2];
+        int32_t page[2];  // as loaded: widening it there would wait for it
+        int64_t at[2], sat[2];
         bool held[2];
         auto look_up = [&](int64_t j0) {
 #pragma unroll
@@ -167,8 +169,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_split(Attend p, int 
             for (int h = 0; h < 2; ++h) {
                 held[h] = page[h] >= 0 && page[h] < p.num_pages;
                 const int64_t in = (j0 + h * 16 + row) & (((int64_t)1 << p.page_bits) - 1);
-                at[h] = page[h] * p.page_stride + in * p.token_stride + part * 16;
-                sat[h] = page[h] * p.scale_page_stride + kv * p.scale_head_stride +
+                const int64_t pg = page[h];
+                at[h] = pg * p.page_stride + in * p.token_stride + part * 16;
+                sat[h] = pg * p.scale_page_stride + kv * p.scale_head_stride +
                          in * p.scale_token_stride;
             }
         };

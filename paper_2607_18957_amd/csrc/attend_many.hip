@@ -13,10 +13,11 @@
 // halves' maxima.
 //
 // Bound by the matrix instructions, the exponentials and LDS about alike: 64
-// keys of 32 rows take a wave's SIMD 1024 cycles of products, as many of
-// vector work, and LDS 256 of its CU's, whose eight waves want it at once.
-// One prompt of 8000 tokens, 32 heads over 8, 8-bit cache: 741 us, 707
-// TFLOP/s (16 rows a workgroup, as for few queries: 2753 us).
+// keys of 32 rows take a wave's SIMD 1024 cycles of products, nearly as many of
+// vector work, and LDS 256, which its eight waves want in turn. One prompt of
+// 8000 tokens, 32 heads over 8, 8-bit cache: 604 us, 868 TFLOP/s (16 rows a
+// workgroup, as for few queries: 2753 us). No register spills: a reload waits
+// for all loads before it, the next tile's too (847 us where some did).
 #include <algorithm>
 
 #include "attend.h"
@@ -67,9 +68,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(Attend p, int row_til
     constexpr int kKRow = kDim + 8, kVRow = kDim + 16;
     __shared__ __attribute__((aligned(16))) T ks[2][kTile * kKRow];
     __shared__ __attribute__((aligned(16))) T vs[2][kTile * kVRow];
-    __shared__ uint8_t state[2][kTile];  // of a key: 1 not there, 2 its values not all finite
+    __shared__ __attribute__((aligned(16))) T apart[2][kTile * kVRow];
+    __shared__ uint8_t state[2][kTile];  // of a key: 1 not there, 2 its values lie in `apart`
 
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 32, half = lane / 32;
+    const int lane = threadIdx.x % 64, row = lane % 32, half = lane / 32;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int kv = blockIdx.x, b = blockIdx.z;
     const int my_part = blockIdx.y % parts_most;
     const int tile0 = row_tiles - 1 - blockIdx.y / parts_most;  // the longest first
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(Attend p, int row_til
         }
 
         // the tile under way: pages of the one after it, words and scales
-        int64_t page[kKeys];
+        int32_t page[kKeys];  // as loaded: widening it here would wait for it
         u32x4 held[kBring];
         uint32_t exponent[kBring];
         bool there[kKeys];
@@ -140,47 +143,61 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(Attend p, int row_til
                 const int k = i % kKeys;
                 if (!there[k]) continue;
                 const int64_t in = (j0 + key_of(i)) & (((int64_t)1 << p.page_bits) - 1);
+                const int64_t at = page[k];
                 held[i] = *reinterpret_cast<const u32x4*>(
-                    (op_of(i) ? p.v : p.k) + kv * p.head_stride + page[k] * p.page_stride +
+                    (op_of(i) ? p.v : p.k) + kv * p.head_stride + at * p.page_stride +
                     in * p.token_stride + word * 16);
                 if (kQuant)
-                    exponent[i] = (op_of(i) ? p.v_scale : p.k_scale)[page[k] * p.scale_page_stride +
+                    exponent[i] = (op_of(i) ? p.v_scale : p.k_scale)[at * p.scale_page_stride +
                                                                     kv * p.scale_head_stride +
                                                                     in * p.scale_token_stride + word / 2];
             }
         };
-        auto keep = [&](int buf) {
+        auto keep = [&](int64_t j0, int buf) {
+            // values that are not finite matter where some row sees a part alone
+            const bool partly = j0 < reach.lo_max || j0 + kTile > reach.hi_min;
 #pragma unroll
             for (int i = 0; i < kBring; ++i) {
-                T* const to = op_of(i) ? &vs[buf][key_of(i) * kVRow] : &ks[buf][key_of(i) * kKRow];
-                bool odd = false;
+                constexpr int kParts = kQuant ? 2 : 1;  // of 8 elements
+                x8 v[kParts];
                 if constexpr (kQuant) {
                     using x2 = typename Vec<T>::x2;
                     const float s = __builtin_bit_cast(float, exponent[i] << 23);
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        x8 v;
+                    for (int w = 0; w < kParts; ++w)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const x2 lo = unpack(held[i][w * 2 + c], s, x2{}, false);
                             const x2 hi = unpack(held[i][w * 2 + c], s, x2{}, true);
-                            v[c * 4] = lo[0];
-                            v[c * 4 + 1] = lo[1];
-                            v[c * 4 + 2] = hi[0];
-                            v[c * 4 + 3] = hi[1];
+                            v[w][c * 4] = lo[0];
+                            v[w][c * 4 + 1] = lo[1];
+                            v[w][c * 4 + 2] = hi[0];
+                            v[w][c * 4 + 3] = hi[1];
                         }
-                        *reinterpret_cast<x8*>(to + word * 16 + w * 8) = v;
-                        odd |= not_finite<T>(v);
-                    }
                 } else {
-                    const x8 v = __builtin_bit_cast(x8, held[i]);
-                    *reinterpret_cast<x8*>(to + word * 8) = v;
-                    odd = not_finite<T>(v);
+                    v[0] = __builtin_bit_cast(x8, held[i]);
                 }
-                // the kWords lanes of a token agree on its state
-                const uint64_t any = __ballot(odd) >> (lane / kWords * kWords) & low_bits(kWords);
+                const auto put = [&](T* to) {
+#pragma unroll
+                    for (int w = 0; w < kParts; ++w)
+                        *reinterpret_cast<x8*>(to + word * 8 * kParts + w * 8) = v[w];
+                };
+                bool mend = false;
+                if (partly) {
+                    bool odd = false;
+#pragma unroll
+                    for (int w = 0; w < kParts; ++w) odd |= not_finite<T>(v[w]);
+                    // the kWords lanes of a token agree
+                    mend = op_of(i) && __ballot(odd) >> (lane / kWords * kWords) & low_bits(kWords);
+                    if (mend) {  // out of the product, to the rows that see it
+                        put(&apart[buf][key_of(i) * kVRow]);
+#pragma unroll
+                        for (int w = 0; w < kParts; ++w) v[w] = x8{};
+                    }
+                }
+                put(op_of(i) ? &vs[buf][key_of(i) * kVRow] : &ks[buf][key_of(i) * kKRow]);
                 if (op_of(i) && word == 0)
-                    state[buf][key_of(i)] = (uint8_t)((there[i % kKeys] ? 0 : 1) | (any ? 2 : 0));
+                    state[buf][key_of(i)] = (uint8_t)((there[i % kKeys] ? 0 : 1) | (mend ? 2 : 0));
             }
         };
 
@@ -251,27 +268,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(Attend p, int row_til
                 return (x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
             };
             __builtin_amdgcn_sched_barrier(0);
-            if (!(edge && odd)) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 4; ++c) {
 #pragma unroll
-                    for (int n = 0; n < kOut; ++n) o[n] = mfma32(value(c, n), w[c], o[n]);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            } else {
-                // keys that are not finite stay out of the product
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int n = 0; n < kOut; ++n) {
-                        x8 v = value(c, n);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (odd >> (c * 16 + e / 4 * 8 + half * 4 + e % 4) & 1) v[e] = (T)0.0f;
-                        o[n] = mfma32(v, w[c], o[n]);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                // and go to the rows that see them alone
+                for (int n = 0; n < kOut; ++n) o[n] = mfma32(value(c, n), w[c], o[n]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (odd) {  // keys that are not finite, for the rows that see them
                 for (uint64_t left = odd; left; left &= left - 1) {
                     const int key = __builtin_ctzll(left), e = key / 8 % 2 * 4 + key % 4;
                     float mine_w = 0;
@@ -281,7 +284,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(Attend p, int row_til
                         for (int x = 0; x < 8; ++x)
                             if (c == key / 16 && x == e) mine_w = (float)w[c][x];
                     const float weight = __shfl(mine_w, key / 4 % 2 * 32 + row);
-                    const T* const at = &vs[buf][key * kVRow + half * 4];
+                    const T* const at = &apart[buf][key * kVRow + half * 4];
                     if (seen >> key & 1)
 #pragma unroll
                         for (int n = 0; n < kOut; ++n)
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(Attend p, int row_til
             look_up(j0 + kTile);
         }
         for (int buf = 0; j0 < end; j0 += kTile, buf ^= 1) {
-            keep(buf);
+            keep(j0, buf);
             if (j0 + kTile < end) {
                 load(j0 + kTile);
                 look_up(j0 + 2 * kTile);
@@ -392,7 +395,7 @@ void launch_dim(const Attend& p, int64_t max_q, int64_t reach, int least_rows,
     // a grid's y counts to 65535; rows past it are taken in turn
     const int64_t row_tiles = std::min<int64_t>((max_q * p.group + kRows - 1) / kRows, 2048);
     const int64_t units = row_tiles * kv_heads * p.seqs, tiles = (reach + kTile - 1) / kTile;
-    // Parts of a sequence by an expected time, us: 64 keys take 256 rows 0.8,
+    // Parts of a sequence by an expected time, us: 64 keys take 256 rows 2,
     // with a workgroup a compute unit; joining costs a launch and its parts'
     // way to memory and back.
     constexpr int64_t kUnits = 256;
@@ -401,7 +404,7 @@ void launch_dim(const Attend& p, int64_t max_q, int64_t reach, int least_rows,
     double best = 1e30;
     for (int64_t n = 1; n <= 32 && (n == 1 || (work.partial && n * 4 <= tiles && units * n <= 4 * kUnits &&
                                                units * n * kFloats <= (int64_t)work.floats)); ++n) {
-        double us = (double)((units * n + kUnits - 1) / kUnits) * ((tiles + n - 1) / n) * 0.8;
+        double us = (double)((units * n + kUnits - 1) / kUnits) * ((tiles + n - 1) / n) * 2;
         if (n > 1) us += 6 + units * n * kFloats * 8 / 3e6;
         if (us < best) best = us, parts = n;
     }
