@@ -464,6 +464,7 @@ void attend_few(const Attend& p, int dtype, bool quant, int dim, int64_t max_q, 
 
 int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
     const char* fn = "ii_attend";
+    const Checks checks;
     CacheRows held;
     int rc = check_cache(fn, c, &held);
     if (rc) return rc;

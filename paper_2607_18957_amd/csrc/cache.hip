@@ -155,6 +155,7 @@ int move(const char* fn, const ii_cache* ca, const ii_tokens* tk, bool write, hi
     if (!ca || !tk) return fail(II_EINVAL, "%s: an argument is NULL", fn);
     const ii_cache& c = *ca;
     const ii_tokens& f = *tk;
+    const Checks checks;
     CacheRows held;
     int rc = check_cache(fn, c, &held);
     if (rc) return rc;

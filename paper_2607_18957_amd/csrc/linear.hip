@@ -871,7 +871,10 @@ int check(const ii_linear_args& a) {
 
 extern "C" int ii_linear(const ii_linear_args* a, hipStream_t stream) {
     if (!a) return ii::fail(II_EINVAL, "ii_linear: args is NULL");
-    if (const int rc = ii::check(*a)) return rc;
+    {
+        const ii::Checks checks;
+        if (const int rc = ii::check(*a)) return rc;
+    }
     if (!a->m || !a->n) return II_OK;
     return a->dtype == II_BF16 ? ii::run<__bf16>(*a, stream) : ii::run<_Float16>(*a, stream);
 }

@@ -3,6 +3,11 @@
 
 namespace ii {
 
+static thread_local AllocInfo found;  // nothing between calls
+
+Checks::Checks() { found = AllocInfo{}; }
+Checks::~Checks() { found = AllocInfo{}; }
+
 int check_rows(const char* fn, const char* what, const void* p, uint64_t rows, uint64_t width,
                uint64_t stride, uint64_t align, Rows* r) {
     *r = Rows{reinterpret_cast<uint64_t>(p), rows, width, stride};
@@ -18,7 +23,11 @@ int check_rows(const char* fn, const char* what, const void* p, uint64_t rows, u
         return fail(II_EOVERFLOW, "%s: %s: %llu rows of %llu bytes at stride %llu", fn, what,
                     (unsigned long long)rows, (unsigned long long)width,
                     (unsigned long long)stride);
-    if (!reachable(alloc_info(r->at), r->at, end))
+    if (found.kind == AllocInfo::kDevice && found.extent && r->at >= found.base &&
+        end <= found.base + found.size)
+        return II_OK;
+    found = alloc_info(r->at);
+    if (!reachable(found, r->at, end))
         return fail(II_EINVAL, "%s: %s [%#llx, +%llu bytes) is not memory the device can reach: "
                     "not inside one device allocation or one pinned host allocation", fn, what,
                     (unsigned long long)r->at, (unsigned long long)span);

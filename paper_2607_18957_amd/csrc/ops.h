@@ -18,6 +18,13 @@ struct Rows {
     uint64_t end() const { return rows && width ? at + (rows - 1) * stride + width : at; }
 };
 
+// One call's checks. The allocation found last is kept until the call's end:
+// ranges of one allocation, one after another, cost one query.
+struct Checks {
+    Checks();
+    ~Checks();
+};
+
 // Form *r and check it: present, aligned, no overflow, inside one allocation
 // the device reaches. Empty ranges pass whatever their address.
 int check_rows(const char* fn, const char* what, const void* p, uint64_t rows, uint64_t width,
