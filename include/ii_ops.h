@@ -163,8 +163,8 @@ int ii_cache_read(const ii_cache* cache, const ii_tokens* to, hipStream_t stream
  *   dtype     of q and out: II_BF16 or II_F16; the cache's, unless that is
  *             II_FP8_E4M3.
  *   heads     query heads, a multiple of cache->heads.
- *   rows      rows of q and out. q_start is read on the device; rows it puts
- *             outside [0, rows) are left out.
+ *   rows      rows of q and out, rows * heads at most 2^30. q_start is read on
+ *             the device; rows it puts outside [0, rows) are left out.
  *   seqs      sequences; lengths has as many, q_start one more.
  *   columns   columns of the page table. Keys past columns * page, and keys
  *             of pages that are negative or not below cache->pages, are not

@@ -476,7 +476,7 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
     if (a.heads < 1 || a.heads % c.heads || a.heads > 65535)
         return fail(II_EINVAL, "%s: %d query heads over %d cache heads", fn, a.heads, c.heads);
     if (a.rows < 0 || a.rows > INT32_MAX || a.seqs < 0 || a.seqs > 65535 || a.max_q < 0 ||
-        a.max_len < 0 || a.window < 0 || a.rows * a.heads > INT32_MAX / 2)
+        a.max_len < 0 || a.window < 0 || a.rows * a.heads > 1 << 30)
         return fail(II_EINVAL, "%s: a size is out of range", fn);
     if (a.columns < 0 || a.columns > ((int64_t)1 << 40) / c.page || a.pages_stride < 0)
         return fail(II_EINVAL, "%s: a page table of %lld columns, stride %lld", fn,

@@ -166,3 +166,9 @@ def test_shapes_that_do_not_fit():
                  lambda: ops.ii_attend(z(1, 2, 64), q, cache, table, n, n)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_attend_refuses_more_rows_than_it_counts():
+    cache = ops._CACHE.pack(*{**CACHE, "pages": 0}.values())
+    args = {**ATTEND, "rows": (1 << 30) // ATTEND["heads"] + 1}
+    assert ops._call_attend(ops._ATTEND.pack(*args.values()), cache, 0) == ii.EINVAL
