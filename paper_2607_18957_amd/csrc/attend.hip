@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_split(Attend p, int 
 #pragma unroll
                 for (int n = 0; n < kOut; ++n) o[n] *= keep;
             }
-            const float base = top == -INFINITY ? 0.0f : top;
+            const float base = top == -INFINITY ? 0.0f : top - lift<T>(0);
             x8 w;
 #pragma unroll
             for (int h = 0; h < 2; ++h)

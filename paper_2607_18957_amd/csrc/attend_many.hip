@@ -240,16 +240,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(Attend p, int row_til
 #pragma unroll
                 for (int e = 0; e < 16; ++e) m = fmaxf(m, s[kb][e]);
             m = max2(m) * by;
-            // sums are taken anew only where a maximum grows by more than 2^8:
-            // weights stay below 256, and every sum keeps 24 bits
-            if (__any(m > top + 8.0f)) {
+            // sums are taken anew only where a maximum grows by more than 2^kGrow:
+            // weights stay below that, and every sum keeps 24 bits
+            constexpr float kGrow = std::is_same_v<T, _Float16> ? 2 : 8;
+            if (__any(m > top + kGrow)) {
                 const float next = fmaxf(top, m), fade = next == -INFINITY ? 1.0f : exp2f(top - next);
                 top = next;
                 sum *= fade;
 #pragma unroll
                 for (int n = 0; n < kOut; ++n) o[n] *= fade;
             }
-            const float base = top == -INFINITY ? 0.0f : top;
+            const float base = top == -INFINITY ? 0.0f : top - lift<T>(kGrow);
             x8 w[4];
             float sums[2] = {};
 #pragma unroll

@@ -611,3 +611,31 @@ def test_attend_many_queries_of_extreme_scores(work):
         q.fill_(by)
         _attend(cache, q, tables, keys, starts, work=work, scale=1.0)
         _attend(cache, q, tables, keys, starts, work=work, scale=-1.0, window=77)
+
+
+@pytest.mark.parametrize("dt,kept", [(F16, F16), (F16, F8), (BF16, BF16)])
+@pytest.mark.parametrize("gap", [14.0, 18.0])
+@pytest.mark.parametrize("queries", [1, 200])
+def test_attend_weights_far_below_the_largest(dt, kept, gap, queries, work):
+    """Many keys whose weights are e^-gap of the largest: alone each is nothing,
+    together they are the result. Four keys (one of each wave's first step of 32)
+    have the largest score and values of zero, all others values of one.
+
+    Scores are exact. The result is off by the rounding of a weight and its own
+    (U each); the exponent's argument, up to 26 in 24 bits, is off by 2^-19, the
+    exponential and the sums by some 2^-19 more (64 additions of 32 keys' sums
+    grow by a power of two at most six times)."""
+    n, dim, page = 65536, 64, 256
+    cache = ops.Cache.empty(n // page, 1, page, dim, kept)
+    k = torch.zeros(n, 1, dim, dtype=dt, device=DEV)
+    v = torch.ones_like(k)
+    k[:128:32, :, 0], v[:128:32] = 1, 0
+    ops.ii_cache_write(cache, k, v, torch.arange(n, device=DEV))
+    q = torch.zeros(queries, 1, dim, dtype=dt, device=DEV)
+    q[..., 0] = gap
+    out = torch.empty_like(q)
+    ops.ii_attend(out, q, cache, torch.arange(n // page, dtype=torch.int32, device=DEV)[None], _i32([n]),
+                  _i32([0, queries]), max_q=queries, scale=1.0)
+    few = (n - queries + 1 + torch.arange(queries, device=DEV) - 4) * math.exp(-gap)
+    want = (few / (few + 4))[:, None, None].double().expand(out.shape)
+    _close(out, want, want * (2 * ops_ref.U[dt] + 2.0 ** -17))
