@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kWaves * 64) void linear_stream(Linear<T> p, uint32
     __shared__ __attribute__((aligned(16))) float red[kWaves * kSums];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
     const int64_t n0 = (int64_t)blockIdx.x * kMine;
-    const int units = (p.k + kUnit - 1) / kUnit, whole = p.k / kUnit;
+    const int units = (int)groups(p.k, kUnit), whole = p.k / kUnit;
 
     const T* wp[kRows];
 #pragma unroll
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(kRowWaves * kKGroups * 64) void linear_shared(Linea
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
     const int rw = wave % kRowWaves, kg = wave / kRowWaves, in_group = threadIdx.x % kGroup;
     const int64_t n0 = (int64_t)blockIdx.x * (kRowWaves * 16) + rw * 16;
-    const int chunks = (p.k + kChunk - 1) / kChunk;
+    const int chunks = (int)groups(p.k, kChunk);
     const int step = kKGroups * gridDim.y, c0 = blockIdx.y * kKGroups + kg;
     const int rounds = (chunks + step - 1) / step;  // alike in every wave
 
@@ -653,8 +653,8 @@ template <class T, bool kGated, int kRows, int kTokens, int kWaves, int kAhead>
 void stream_launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
     constexpr int kMine = kRows * 16 / (kGated ? 2 : 1);
     constexpr uint64_t kSums = kRows * kTokens * 256;
-    const uint32_t tiles = (p.n + kMine - 1) / kMine;
-    const int units = (p.k + kUnit - 1) / kUnit;
+    const uint32_t tiles = (uint32_t)groups(p.n, kMine);
+    const int units = (int)groups(p.k, kUnit);
     // workgroups that share a tile's k: to fill the compute units, each wave
     // left with two rounds of loads or more
     uint32_t split = 1;
@@ -667,7 +667,7 @@ void stream_launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
 
 template <class T, bool kGated, int kRows, int kTokens, int kAhead>
 void stream_waves(const Linear<T>& p, const Work& work, hipStream_t stream) {
-    const int64_t tiles = (p.n + 15) / 16, units = (p.k + kUnit - 1) / kUnit;
+    const int64_t tiles = groups(p.n, 16), units = groups(p.k, kUnit);
     if (tiles <= 512 && units >= 32)
         stream_launch<T, kGated, kRows, kTokens, kTokens < 4 ? 16 : 8, kAhead>(p, work, stream);
     else if (tiles <= 2048 && units >= 16)
@@ -680,8 +680,8 @@ template <class T, bool kGated, int kTokens>
 void shared_launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
     constexpr int kCols = kRowWaves * 16;
     constexpr uint64_t kAll = (uint64_t)kCols * kTokens * 16 * (kGated ? 2 : 1);
-    const uint32_t tiles = (p.n + kCols - 1) / kCols;
-    const uint32_t chunks = (p.k + shared_chunk(kGated) - 1) / shared_chunk(kGated);
+    const uint32_t tiles = (uint32_t)groups(p.n, kCols);
+    const uint32_t chunks = (uint32_t)groups(p.k, shared_chunk(kGated));
     // as many workgroups as compute units, each wave with a chunk or more
     uint32_t split = 1;
     if (work.partial && tiles < kUnits)
@@ -713,11 +713,11 @@ struct Choice {
 };
 Choice choose_tile(int64_t m, int64_t n, int64_t k, bool gated, const Work& work, int shapes) {
     Choice best;
-    const int64_t steps = (k + kTileK - 1) / kTileK;
+    const int64_t steps = groups(k, kTileK);
     for (int i = 0; i < shapes; ++i) {
         const Shape& s = kShapes[i];
         const int64_t cols = gated ? s.n / 2 : s.n;
-        const int64_t tiles = ((m + s.m - 1) / s.m) * ((n + cols - 1) / cols);
+        const int64_t tiles = groups(m, s.m) * groups(n, cols);
         for (int64_t split = 1; split <= 16; ++split) {
             if (split > 1 && (!s.splits || !work.partial || tiles * split > kUnits ||
                               split * 2 > steps ||
@@ -735,7 +735,7 @@ Choice choose_tile(int64_t m, int64_t n, int64_t k, bool gated, const Work& work
 template <class T, bool kGated, int kM, int kN, int kStages, bool kDirect>
 void tile_launch(const Linear<T>& p, const Work& work, uint32_t split, hipStream_t stream) {
     constexpr int kCols = kGated ? kN / 2 : kN;
-    const int tm = (p.m + kM - 1) / kM, tn = (p.n + kCols - 1) / kCols;
+    const int tm = (int)groups(p.m, kM), tn = (int)groups(p.n, kCols);
     const int64_t tiles = (int64_t)tm * tn;
     const int64_t resident = kM == 64 ? 2 * kUnits : kUnits;  // workgroups the card holds at once
     linear_tile<T, kGated, kM, kN, kStages, kDirect>

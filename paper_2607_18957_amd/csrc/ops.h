@@ -54,6 +54,9 @@ struct CacheRows {
 };
 int check_cache(const char* fn, const ii_cache& c, CacheRows* held);
 
+// Groups of `size` that hold n things; in 64 bits, as n + size - 1 need not fit n's type.
+constexpr int64_t groups(int64_t n, int64_t size) { return (n + size - 1) / size; }
+
 inline bool half_type(int32_t dtype) { return dtype == II_BF16 || dtype == II_F16; }
 
 // Scratch of split work: counters first, each zero between calls, then the

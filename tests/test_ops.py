@@ -639,3 +639,35 @@ def test_attend_weights_far_below_the_largest(dt, kept, gap, queries, work):
     few = (n - queries + 1 + torch.arange(queries, device=DEV) - 4) * math.exp(-gap)
     want = (few / (few + 4))[:, None, None].double().expand(out.shape)
     _close(out, want, want * (2 * ops_ref.U[dt] + 2.0 ** -17))
+
+
+@pytest.mark.parametrize("m", [2, 8])
+def test_linear_longest_rows(m, work):
+    """k within 63 of 2^31, rows that broadcast: x is -1, 1, -1, 1, .., but 2 in
+    its last three places, against ones: 5, exactly, in any order of pairs."""
+    k = (1 << 31) - 8
+    x = torch.ones(1, k, dtype=BF16, device=DEV)
+    x[0, ::2] = -1
+    x[0, -3:] = 2
+    w = torch.ones(1, k, dtype=BF16, device=DEV)
+    for n, out_work in ((3, work), (130, None)):
+        out = torch.empty(m, n, dtype=F32, device=DEV)
+        ops.ii_linear(out, x.expand(m, k), w.expand(n, k), work=out_work)
+        assert bool((out == 5).all())
+
+
+def test_linear_most_columns_and_most_rows():
+    """n, then m, of 2^31 - 1: whole numbers, exact."""
+    most = (1 << 31) - 1
+    ones = torch.ones(1, 8, dtype=BF16, device=DEV)
+    add = torch.empty(most, dtype=BF16, device=DEV)
+    step = 1 << 28
+    for i in range(0, most, step):
+        part = add[i:i + step]
+        part.copy_(torch.arange(i, i + part.numel(), device=DEV) % 251 - 120)  # whole, below 2^8: exact
+    out = torch.empty_like(add)
+    ops.ii_linear(out[None], ones, ones.expand(most, 8), bias=add)
+    assert torch.equal(out - 8, add)
+    out.zero_()
+    ops.ii_linear(out[:, None], ones.expand(most, 8), ones, residual=add[:, None])
+    assert torch.equal(out - 8, add)
