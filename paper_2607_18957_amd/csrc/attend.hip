@@ -527,7 +527,9 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
     p.pages_stride = a.pages_stride;
     p.capacity = a.columns * c.page;
     p.rows = a.rows;
-    p.window = a.window;
+    // lengths are 32-bit: a window of 2^31 hides nothing, and the sums of positions
+    // and windows below stay far from 64 bits' ends
+    p.window = a.window <= INT32_MAX ? a.window : 0;
     p.num_pages = c.pages;
     p.seqs = (int32_t)a.seqs;
     p.heads = a.heads;

@@ -671,3 +671,17 @@ def test_linear_most_columns_and_most_rows():
     out.zero_()
     ops.ii_linear(out[:, None], ones.expand(most, 8), ones, residual=add[:, None])
     assert torch.equal(out - 8, add)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31, 2 ** 63 - 1])
+@pytest.mark.parametrize("keys,queries", [([5, 300, 0], [9, 1, 3]), ([5, 200, 150], [40, 60, 150]),
+                                          ([20000], [1])])
+def test_attend_windows_that_hide_nothing(keys, queries, window, work):
+    """Windows as long as a length can be, up to the largest number: as none, in
+    both kernels, with more queries than keys too."""
+    b = _batch(_gen(8), keys, queries, 8, 2, 128, 16)
+    want = _attend(*b, work=work)
+    out = torch.empty_like(b[1])
+    ops.ii_attend(out, b[1], b[0], _i32(b[2]), _i32(keys), _i32(b[4]), max_q=max(queries), window=window,
+                  work=work)
+    assert torch.equal(out, want)
