@@ -409,7 +409,8 @@ void launch_dim(const Attend& p, int64_t max_q, int64_t reach, int least_rows,
         if (n > 1) us += 6 + units * n * kFloats * 8 / 3e6;
         if (us < best) best = us, parts = n;
     }
-    const int part_keys = (int)std::min<int64_t>((tiles + parts - 1) / parts * kTile, INT32_MAX / 2);
+    // of a tile at least: a table without columns has none
+    const int part_keys = (int)std::clamp<int64_t>((tiles + parts - 1) / parts * kTile, kTile, INT32_MAX / 2);
     attend_rows<T, kQuant, kDim>
         <<<dim3(kv_heads, (uint32_t)(row_tiles * parts), p.seqs), kThreads, 0, stream>>>(
             p, (int)row_tiles, (int)parts, part_keys, least_rows, work.partial);

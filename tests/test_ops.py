@@ -685,3 +685,16 @@ def test_attend_windows_that_hide_nothing(keys, queries, window, work):
     ops.ii_attend(out, b[1], b[0], _i32(b[2]), _i32(keys), _i32(b[4]), max_q=max(queries), window=window,
                   work=work)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("queries", [1, 300])
+@pytest.mark.parametrize("max_len", [0, 500])
+def test_attend_without_columns(queries, max_len, work):
+    """A page table of no columns: no key is seen, in both kernels."""
+    cache, q, _, _, starts = _batch(_gen(9), [500, 500], [queries, 1], 8, 2, 128, 16)
+    none = torch.empty(2, 0, dtype=torch.int32, device=DEV)
+    for window in (0, 7):
+        out = torch.full_like(q, 77.0)
+        ops.ii_attend(out, q, cache, none, _i32([500, 500]), _i32(starts), max_q=queries, max_len=max_len,
+                      window=window, work=work)
+        assert not out.any()
