@@ -17,7 +17,8 @@
  *     use. A call leaves it fit for the next one on the same stream; calls
  *     that may overlap on different streams need scratch of their own. NULL
  *     (0 bytes) means that nothing is split, which is slower for few rows.
- *     II_WORK_BYTES is as much as any call makes use of. The same inputs,
+ *     II_WORK_BYTES is as much as any call makes use of; that much of it may
+ *     not meet what else the call reads or writes (II_EOVERLAP). The same inputs,
  *     strides and work_bytes give the same bits.
  */
 #ifndef II_OPS_H

@@ -486,7 +486,7 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
         return fail(II_EINVAL, "%s: %lld rows for %lld sequences without q_start", fn,
                     (long long)a.rows, (long long)a.seqs);
     if (!a.rows || !a.seqs) return II_OK;
-    Rows q, out, table, lengths, starts;
+    Rows q, out, table, lengths, starts, scratch;
     if ((rc = check_heads(fn, "out", a.out, a.rows, a.heads, c.dim, a.out_row_stride,
                           a.out_head_stride, 2, true, &out)) ||
         (rc = check_heads(fn, "q", a.q, a.rows, a.heads, c.dim, a.q_row_stride, a.q_head_stride, 2,
@@ -496,13 +496,17 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
         (rc = check_rows(fn, "lengths", a.lengths, 1, (uint64_t)a.seqs * 4, 0, 4, &lengths)) ||
         (rc = check_rows(fn, "q_start", a.q_start, a.q_start ? 1 : 0, ((uint64_t)a.seqs + 1) * 4, 0,
                          4, &starts)) ||
-        (rc = check_work(fn, a.work, a.work_bytes)) || (rc = check_apart(fn, "q", out, q)) ||
-        (rc = check_apart(fn, "pages", out, table)) ||
-        (rc = check_apart(fn, "lengths", out, lengths)) ||
-        (rc = check_apart(fn, "q_start", out, starts)))
+        (rc = check_work(fn, a.work, a.work_bytes, &scratch)) ||
+        (rc = check_apart(fn, "work", out, scratch)))
         return rc;
-    for (const Rows& r : held.all)
-        if ((rc = check_apart(fn, "the cache", out, r))) return rc;
+    for (const Rows& written : {out, scratch}) {
+        if ((rc = check_apart(fn, "q", written, q)) || (rc = check_apart(fn, "pages", written, table)) ||
+            (rc = check_apart(fn, "lengths", written, lengths)) ||
+            (rc = check_apart(fn, "q_start", written, starts)))
+            return rc;
+        for (const Rows& r : held.all)
+            if ((rc = check_apart(fn, "the cache", written, r))) return rc;
+    }
     const int64_t size = quant ? 1 : 2;
     Attend p;
     p.q = static_cast<const uint8_t*>(a.q);

@@ -835,10 +835,12 @@ int check(const ii_linear_args& a) {
     if (!a.m || !a.n) return II_OK;
     const uint64_t m = a.m, n = a.n, k = a.k, size = 2, osize = a.out_dtype == II_F32 ? 4 : 2;
     static const char* const kResidual = "residual";
-    Rows out, r;
+    Rows out, scratch, r;
     int rc = check_rows(fn, "out", a.out, m, n * osize, (m > 1 ? a.out_stride : 0) * osize, osize,
                         &out);
-    if (rc) return rc;
+    if (rc || (rc = check_work(fn, a.work, a.work_bytes, &scratch)) ||
+        (rc = check_apart(fn, "work", out, scratch)))
+        return rc;
     const struct {
         const char* what;
         const void* p;
@@ -856,14 +858,14 @@ int check(const ii_linear_args& a) {
         if (__builtin_mul_overflow(in.rows > 1 ? in.stride : 0, size, &stride))
             return fail(II_EOVERFLOW, "%s: the stride of %s", fn, in.what);
         rc = check_rows(fn, in.what, in.p, in.rows, in.width * size, stride, size, &r);
-        if (rc) return rc;
+        if (rc || (rc = check_apart(fn, in.what, scratch, r))) return rc;
         if (in.what == kResidual && in.p == a.out && a.out_dtype == a.dtype &&
             (m == 1 || a.residual_stride == a.out_stride))
             continue;  // each element is read by the lane that then writes it
         rc = check_apart(fn, in.what, out, r);
         if (rc) return rc;
     }
-    return check_work(fn, a.work, a.work_bytes);
+    return II_OK;
 }
 
 }  // namespace

@@ -137,10 +137,12 @@ int check_cache(const char* fn, const ii_cache& c, CacheRows* held) {
     return II_OK;
 }
 
-int check_work(const char* fn, const void* work, uint64_t bytes) {
+int check_work(const char* fn, const void* work, uint64_t bytes, Rows* r) {
+    *r = Rows{};
     if (!work && !bytes) return II_OK;
-    Rows r;
-    return check_rows(fn, "work", work, 1, bytes, 0, 16, &r);
+    const int rc = check_rows(fn, "work", work, 1, bytes, 0, 16, r);
+    if (r->width > II_WORK_BYTES) r->width = II_WORK_BYTES;
+    return rc;
 }
 
 int launched(const char* fn) {

@@ -63,7 +63,8 @@ inline bool half_type(int32_t dtype) { return dtype == II_BF16 || dtype == II_F1
 // partial results.
 constexpr uint64_t kWorkCounters = 16384;
 constexpr uint64_t kWorkHead = kWorkCounters * 4;
-int check_work(const char* fn, const void* work, uint64_t bytes);
+// *r: what a call may write of it, to be kept apart from its other operands.
+int check_work(const char* fn, const void* work, uint64_t bytes, Rows* r);
 
 int launched(const char* fn);
 

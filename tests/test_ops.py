@@ -698,3 +698,67 @@ def test_attend_without_columns(queries, max_len, work):
         ops.ii_attend(out, q, cache, none, _i32([500, 500]), _i32(starts), max_q=queries, max_len=max_len,
                       window=window, work=work)
         assert not out.any()
+
+
+def _apart_from_work(call, tensors):
+    """call(work, **tensors) refuses work that meets any one of the tensors, and
+    takes work that ends where the tensor starts or lies before it in one buffer."""
+    for what, t in tensors.items():
+        raw = t.contiguous().view(torch.uint8).flatten()
+        buf = torch.zeros((1 << 20) + raw.numel() + 256, dtype=torch.uint8, device=DEV)
+        for first in (0, 1 << 20):
+            held = buf[first:first + raw.numel()]
+            held.copy_(raw)
+            moved = held.view(t.dtype).view(t.shape)
+            last = first + raw.numel() - 1 & ~15          # the last aligned place inside
+            for a, b in ((first, first + 4096), (last, last + (1 << 17)), (max(0, first - 4096), first + 16)):
+                work = buf[a:b]
+                with pytest.raises(ii.IIError) as e:
+                    call(work, **{**tensors, what: moved})
+                assert e.value.name == "II_EOVERLAP", (what, first, a, b)
+            assert torch.equal(held, raw), what
+        buf[:1 << 20] = 0
+        call(buf[:1 << 20], **{**tensors, what: moved})   # ends where the tensor starts
+
+
+def test_linear_work_is_apart():
+    g = _gen(11)
+    m, n, k = 3, 64, 9000
+    x, w, w2 = _normal(g, m, k), _normal(g, n, k, std=k ** -0.5), _normal(g, n, k, std=k ** -0.5)
+    b, b2, r = _normal(g, 1, n)[0].contiguous(), _normal(g, 1, n)[0].contiguous(), _normal(g, m, n)
+    want, bound = ops_ref.linear(x, w, BF16, b, w2, b2, r)
+
+    def call(work, out, x, w, w2, bias, bias2, residual):
+        ops.ii_linear(out, x, w, w2=w2, bias=bias, bias2=bias2, residual=residual, work=work)
+        _close(out, want, bound)
+
+    _apart_from_work(call, dict(out=torch.zeros(m, n, dtype=BF16, device=DEV), x=x, w=w, w2=w2, bias=b,
+                                bias2=b2, residual=r))
+
+
+@pytest.mark.parametrize("kept", [F8, BF16])
+def test_attend_work_is_apart(kept):
+    cache, q, tables, keys, starts = _batch(_gen(12), [3000, 40], [1, 2], 8, 2, 128, 64, BF16, kept)
+    want, far, _ = ops_ref.attend(q, cache, tables, keys, starts)
+    held = dict(k=cache.k, v=cache.v)
+    if kept == F8:
+        held.update(k_scale=cache.k_scale, v_scale=cache.v_scale)
+
+    def call(work, out, q, pages, lengths, q_start, **held):
+        ops.ii_attend(out, q, ops.Cache(**held), pages, lengths, q_start, max_q=2, work=work)
+        _close(out, want, far)
+
+    _apart_from_work(call, dict(out=torch.zeros_like(q), q=q, pages=_i32(tables), lengths=_i32(keys),
+                                q_start=_i32(starts), **held))
+
+
+def test_work_past_what_a_call_uses(work):
+    """Only the first WORK_BYTES of scratch are a call's: operands may follow."""
+    g = _gen(13)
+    x, w = _normal(g, 3, 9000), _normal(g, 64, 9000, std=9000 ** -0.5)
+    arena = torch.zeros(ops.WORK_BYTES + x.numel() * 2, dtype=torch.uint8, device=DEV)
+    at = arena[ops.WORK_BYTES:].view(BF16).view(3, 9000)
+    at.copy_(x)
+    out = torch.empty(3, 64, dtype=BF16, device=DEV)
+    ops.ii_linear(out, at, w, work=arena)
+    _close(out, *ops_ref.linear(x, w, BF16))
