@@ -134,7 +134,8 @@ typedef struct ii_tokens {
  * leave the scale alone. For II_F16 tokens no value above 61440 is kept (the
  * next, 65536, does not fit the type).
  * Tokens whose slot is negative or past the last page are left out. Two
- * tokens of one call must not have the same slot.
+ * tokens of one call must not have the same slot. The cache's arrays may lie in
+ * one buffer in any order of axes, but not meet (II_EOVERLAP).
  */
 int ii_cache_write(const ii_cache* cache, const ii_tokens* from, hipStream_t stream);
 

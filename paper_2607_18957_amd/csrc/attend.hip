@@ -466,7 +466,7 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
     const char* fn = "ii_attend";
     const Checks checks;
     CacheRows held;
-    int rc = check_cache(fn, c, &held);
+    int rc = check_cache(fn, c, false, &held);
     if (rc) return rc;
     if (!half_type(a.dtype)) return fail(II_EINVAL, "%s: dtype %d", fn, a.dtype);
     const bool quant = c.dtype == II_FP8_E4M3;

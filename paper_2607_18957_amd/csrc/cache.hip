@@ -157,7 +157,7 @@ int move(const char* fn, const ii_cache* ca, const ii_tokens* tk, bool write, hi
     const ii_tokens& f = *tk;
     const Checks checks;
     CacheRows held;
-    int rc = check_cache(fn, c, &held);
+    int rc = check_cache(fn, c, write, &held);
     if (rc) return rc;
     if (!half_type(f.dtype)) return fail(II_EINVAL, "%s: dtype %d", fn, f.dtype);
     if (c.dtype != II_FP8_E4M3 && c.dtype != f.dtype)

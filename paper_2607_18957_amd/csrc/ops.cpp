@@ -1,6 +1,8 @@
 // Argument checks of the operators.
 #include "ops.h"
 
+#include <algorithm>
+
 namespace ii {
 
 static thread_local AllocInfo found;  // nothing between calls
@@ -46,8 +48,8 @@ int check_apart(const char* fn, const char* what, const Rows& w, const Rows& r) 
 }
 
 int check_span(const char* fn, const char* what, const Axis* axes, int n, uint64_t width,
-               bool apart, uint64_t* span) {
-    Axis by[4];
+               bool apart, uint64_t* span, Nest* nest) {
+    Axis by[3];
     int live = 0;
     for (int i = 0; i < n; ++i) {
         if (axes[i].count <= 1) continue;
@@ -67,7 +69,37 @@ int check_span(const char* fn, const char* what, const Axis* axes, int n, uint64
             return fail(II_EOVERFLOW, "%s: the extent of %s", fn, what);
     }
     *span = end;
+    if (nest) {
+        nest->width = width;
+        nest->axes = live;
+        std::copy(by, by + live, nest->by);
+    }
     return II_OK;
+}
+
+bool nests_meet(const Nest& a, const Nest& b) {
+    const auto extent = [](const Nest& x) {
+        uint64_t e = x.width;
+        for (int i = 0; i < x.axes; ++i) e += (uint64_t)(x.by[i].count - 1) * x.by[i].stride;
+        return e;
+    };
+    // distances, as the arrays may end past the last address
+    if (b.at >= a.at ? b.at - a.at >= extent(a) : a.at - b.at >= extent(b)) return false;
+    if (!a.axes || !b.axes || a.by[a.axes - 1].stride != b.by[b.axes - 1].stride) return true;
+    // Place i of a against place j of b along this axis: what lies inside a
+    // place is shorter than the stride, so it meets that of i - j = q or q + 1,
+    // b being q strides and a part of one after a.
+    Nest x = a, y = b;
+    const Axis& ax = a.by[--x.axes];
+    const Axis& bx = b.by[--y.axes];
+    const int64_t s = ax.stride, d = (int64_t)(b.at - a.at);  // less than 2^63 apart
+    const int64_t q = d >= 0 ? d / s : -((-d + s - 1) / s);
+    for (int64_t i = q; i <= q + 1; ++i) {
+        if (i >= ax.count || i <= -bx.count) continue;
+        x.at = a.at + (uint64_t)(i * s);
+        if (nests_meet(x, y)) return true;
+    }
+    return false;
 }
 
 int check_heads(const char* fn, const char* what, const void* p, int64_t tokens, int64_t heads,
@@ -94,7 +126,7 @@ int check_heads(const char* fn, const char* what, const void* p, int64_t tokens,
     return check_rows(fn, what, p, 1, span, 0, 16, r);
 }
 
-int check_cache(const char* fn, const ii_cache& c, CacheRows* held) {
+int check_cache(const char* fn, const ii_cache& c, bool written, CacheRows* held) {
     const bool quant = c.dtype == II_FP8_E4M3;
     if (!quant && !half_type(c.dtype)) return fail(II_EINVAL, "%s: cache of type %d", fn, c.dtype);
     if (c.heads < 1) return fail(II_EINVAL, "%s: cache of %d heads", fn, c.heads);
@@ -110,6 +142,7 @@ int check_cache(const char* fn, const ii_cache& c, CacheRows* held) {
     const void* const at[4] = {c.k, c.v, c.k_scale, c.v_scale};
     const int arrays = quant ? 4 : 2;
     uint64_t span[4];
+    Nest nest[4];
     for (int i = 0; i < arrays; ++i) {
         Axis axes[3] = {{c.pages, c.page_stride}, {c.heads, c.head_stride}, {c.page, c.token_stride}};
         if (i >= 2) {
@@ -126,8 +159,12 @@ int check_cache(const char* fn, const ii_cache& c, CacheRows* held) {
                             "bytes", fn, what[i], (long long)a.stride, (long long)align);
         }
         const int rc = check_span(fn, what[i], axes, 3, i < 2 ? c.dim * size : c.dim / 32, true,
-                                  &span[i]);
+                                  &span[i], &nest[i]);
         if (rc) return rc;
+        nest[i].at = reinterpret_cast<uint64_t>(at[i]);
+        for (int j = 0; j < i && written; ++j)
+            if (at[i] && at[j] && nests_meet(nest[i], nest[j]))
+                return fail(II_EOVERLAP, "%s: %s and %s meet", fn, what[j], what[i]);
     }
     for (int i = 0; i < arrays; ++i) {
         const int rc = check_rows(fn, what[i], at[i], 1, span[i], 0, i < 2 ? 16 : c.dim / 32,

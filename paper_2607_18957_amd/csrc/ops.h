@@ -36,12 +36,24 @@ int check_apart(const char* fn, const char* what, const Rows& written, const Row
 
 // [count][stride] axes around a contiguous row of `width` bytes, strides in
 // bytes: *span receives the bytes from the first to the last, and what no two
-// rows share (`apart`) is required of memory that is written.
+// rows share (`apart`) is required of memory that is written. *nest (if not
+// NULL) receives the axes of more than one place, the least stride first.
 struct Axis {
     int64_t count, stride;
 };
+struct Nest {
+    uint64_t at, width;
+    int axes;
+    Axis by[3];
+};
 int check_span(const char* fn, const char* what, const Axis* axes, int n, uint64_t width,
-               bool apart, uint64_t* span);
+               bool apart, uint64_t* span, Nest* nest = nullptr);
+
+// Whether two arrays, each with rows apart, share a byte. Exact where strides
+// agree from the largest down to where one array's rows lie within the other's
+// gaps (arrays of one shape in one buffer, in any order of axes); where they do
+// not agree, arrays whose extents meet count as meeting.
+bool nests_meet(const Nest& a, const Nest& b);
 
 // [tokens][heads][dim] of `size`-byte elements at strides in elements.
 int check_heads(const char* fn, const char* what, const void* p, int64_t tokens, int64_t heads,
@@ -52,7 +64,7 @@ int check_heads(const char* fn, const char* what, const void* p, int64_t tokens,
 struct CacheRows {
     Rows all[4];
 };
-int check_cache(const char* fn, const ii_cache& c, CacheRows* held);
+int check_cache(const char* fn, const ii_cache& c, bool written, CacheRows* held);
 
 // Groups of `size` that hold n things; in 64 bits, as n + size - 1 need not fit n's type.
 constexpr int64_t groups(int64_t n, int64_t size) { return (n + size - 1) / size; }

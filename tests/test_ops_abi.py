@@ -172,3 +172,95 @@ def test_attend_refuses_more_rows_than_it_counts():
     cache = ops._CACHE.pack(*{**CACHE, "pages": 0}.values())
     args = {**ATTEND, "rows": (1 << 30) // ATTEND["heads"] + 1}
     assert ops._call_attend(ops._ATTEND.pack(*args.values()), cache, 0) == ii.EINVAL
+
+
+def _places(at, width, *axes):
+    """First bytes of the rows of an array: (count, stride in bytes) of its axes."""
+    rows = [at]
+    for count, stride in axes:
+        rows = [r + i * stride for r in rows for i in range(count)]
+    return [(r, r + width) for r in rows]
+
+
+def _cache_arrays(c):
+    """Byte ranges of the arrays of a cache (CACHE's fields)."""
+    size = 1 if c["dtype"] == 3 else 2
+    n = (c["pages"], c["heads"], c["page"])
+    data = [(k, s * size) for k, s in zip(n, (c["page_stride"], c["head_stride"], c["token_stride"]))]
+    out = [_places(c[x], c["dim"] * size, *data) for x in ("k", "v")]
+    if size == 1:
+        scale = list(zip(n, (c["scale_page_stride"], c["scale_head_stride"], c["scale_token_stride"])))
+        out += [_places(c[x], c["dim"] // 32, *scale) for x in ("k_scale", "v_scale")]
+    return out
+
+
+def _meet(arrays):
+    marked = set()
+    for rows in arrays:
+        mine = {b for first, end in rows for b in range(first, end)}
+        if marked & mine:
+            return True
+        marked |= mine
+    return False
+
+
+def test_written_cache_arrays_are_apart():
+    """Arrays of one buffer at random distances, in random orders of axes, against
+    the bytes they hold: ii_cache_write refuses those that meet and no others;
+    ii_cache_read, which writes none of them, refuses none."""
+    import random
+    rng = random.Random(5)
+    tokens = ops._TOKENS.pack(*TOKENS.values())
+    met = apart = 0
+    for _ in range(1500):
+        quant = rng.random() < 0.5
+        n = [rng.choice([1, 1, 2, 3]), rng.choice([1, 2, 3]), rng.choice([1, 2, 4])]
+        size = 1 if quant else 2
+        order, strides, span = rng.sample(range(3), 3), [0, 0, 0], 64 * size
+        scales, sspan = [0, 0, 0], 2
+        for axis in order:      # the innermost first; room for a second array or not
+            strides[axis] = span * rng.choice([1, 1, 2]) + 16 * rng.choice([0, 0, 1, 3])
+            scales[axis] = sspan * rng.choice([1, 1, 2])
+            span = strides[axis] * (n[axis] - 1) + span
+            sspan = scales[axis] * (n[axis] - 1) + sspan
+        if quant and rng.random() < 0.5:    # scales behind the codes of each page
+            strides[0] = scales[0] = max(strides[0], -(-(span + 2 * sspan) // 16) * 16)
+        base = 1 << 40
+        c = {**CACHE, "dtype": 3 if quant else 5, "pages": n[0], "heads": n[1], "page": n[2], "k": base,
+             "v": base + 16 * rng.randint(-span // 8, span // 8),
+             "page_stride": strides[0] // size, "head_stride": strides[1] // size,
+             "token_stride": strides[2] // size}
+        if rng.random() < 0.4:
+            c["v"] = base + rng.choice(strides) // 32 * 16
+        if quant:
+            c.update(scale_page_stride=scales[0], scale_head_stride=scales[1], scale_token_stride=scales[2],
+                     k_scale=base + rng.choice([span, 1 << 20, rng.randint(0, span) & ~1]))
+            c["v_scale"] = c["k_scale"] + rng.choice([sspan, 1 << 20, scales[1] // 4 * 2, 0])
+        cache = ops._CACHE.pack(*c.values())
+        write, read = (ii.ERRNAMES[f(cache, tokens, 0)] for f in (ops._call_write, ops._call_read))
+        assert read == "II_EINVAL", (read, c)       # not memory of any device
+        arrays = _cache_arrays(c)
+        # what the strides do not tell apart may be refused: scales among codes
+        if _meet(arrays):
+            met += 1
+            assert write == "II_EOVERLAP", c
+        elif not (_meet([*arrays[:2]]) or quant and any(
+                min(a)[0] < max(s)[1] and min(s)[0] < max(a)[1] for a in arrays[:2] for s in arrays[2:])):
+            apart += 1
+            assert write == "II_EINVAL", c
+    assert met > 300 and apart > 300, (met, apart)
+
+
+@pytest.mark.parametrize("layout", ["pages", "heads", "tokens", "positions"])
+def test_keys_and_values_of_one_buffer(layout):
+    """k and v side by side in every place of an axis are apart; one array twice is not."""
+    p, h, t, d = 3, 2, 4, 64
+    a = {"pages": (2 * h * t * d, t * d, d, h * t * d), "heads": (2 * h * t * d, 2 * t * d, d, t * d),
+         "tokens": (2 * h * t * d, t * 2 * d, 2 * d, d), "positions": (2 * t * h * d, 2 * d, 2 * h * d, d)}[layout]
+    c = {**CACHE, "dtype": 5, "pages": p, "heads": h, "page": t, "v": CACHE["k"] + 2 * a[3],
+         "page_stride": a[0], "head_stride": a[1], "token_stride": a[2]}
+    tokens = ops._TOKENS.pack(*TOKENS.values())
+    for v, name in ((c["v"], "II_EINVAL"), (c["k"], "II_EOVERLAP"), (c["v"] - 16, "II_EOVERLAP"),
+                    (c["k"] + 2 * a[1], "II_EOVERLAP"), (c["k"] + 2 * a[0], "II_EOVERLAP"),
+                    (c["k"] + 2 * p * a[0], "II_EINVAL")):
+        _refused(ops._call_write(ops._CACHE.pack(*{**c, "v": v}.values()), tokens, 0), name)
