@@ -167,6 +167,7 @@ int move(const char* fn, const ii_cache* ca, const ii_tokens* tk, bool write, hi
         return fail(II_EINVAL, "%s: %lld tokens", fn, (long long)f.tokens);
     if (!f.tokens) return II_OK;
     Rows slots, rows[2];
+    Nest nest[2];
     rc = check_rows(fn, "slots", f.slots, 1, (uint64_t)f.tokens * 8, 0, 8, &slots);
     if (rc) return rc;
     const int64_t ts[2] = {f.k_token_stride, f.v_token_stride};
@@ -175,7 +176,7 @@ int move(const char* fn, const ii_cache* ca, const ii_tokens* tk, bool write, hi
     const char* const what[2] = {"k", "v"};
     for (int i = 0; i < 2; ++i) {
         rc = check_heads(fn, what[i], at[i], f.tokens, c.heads, c.dim, ts[i], hs[i], 2, !write,
-                         &rows[i]);
+                         &rows[i], &nest[i]);
         if (rc) return rc;
     }
     for (int i = 0; i < 2; ++i) {
@@ -188,7 +189,7 @@ int move(const char* fn, const ii_cache* ca, const ii_tokens* tk, bool write, hi
     if (write)
         for (const Rows& r : held.all)
             if ((rc = check_apart(fn, "slots", r, slots))) return rc;
-    if (!write && (rc = check_apart(fn, "v", rows[0], rows[1]))) return rc;
+    if (!write && nests_meet(nest[0], nest[1])) return fail(II_EOVERLAP, "%s: k and v meet", fn);
     Cache d;
     const int size = c.dtype == II_FP8_E4M3 ? 1 : 2;
     d.at[0] = static_cast<uint8_t*>(c.k);

@@ -104,7 +104,7 @@ bool nests_meet(const Nest& a, const Nest& b) {
 
 int check_heads(const char* fn, const char* what, const void* p, int64_t tokens, int64_t heads,
                 int64_t dim, int64_t token_stride, int64_t head_stride, int size, bool written,
-                Rows* r) {
+                Rows* r, Nest* nest) {
     if (!tokens) {
         *r = Rows{};
         return II_OK;
@@ -119,8 +119,9 @@ int check_heads(const char* fn, const char* what, const void* p, int64_t tokens,
     const Axis axes[2] = {{tokens, ts}, {heads, hs}};
     uint64_t token, span;
     int rc = check_span(fn, what, axes + 1, 1, dim * size, written, &token);
-    if (!rc) rc = check_span(fn, what, axes, 2, dim * size, written, &span);
+    if (!rc) rc = check_span(fn, what, axes, 2, dim * size, written, &span, nest);
     if (rc) return rc;
+    if (nest) nest->at = reinterpret_cast<uint64_t>(p);
     // tokens one after another, or one range
     if (tokens > 1 && token <= (uint64_t)ts) return check_rows(fn, what, p, tokens, token, ts, 16, r);
     return check_rows(fn, what, p, 1, span, 0, 16, r);

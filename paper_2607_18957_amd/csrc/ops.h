@@ -58,7 +58,7 @@ bool nests_meet(const Nest& a, const Nest& b);
 // [tokens][heads][dim] of `size`-byte elements at strides in elements.
 int check_heads(const char* fn, const char* what, const void* p, int64_t tokens, int64_t heads,
                 int64_t dim, int64_t token_stride, int64_t head_stride, int size, bool written,
-                Rows* r);
+                Rows* r, Nest* nest = nullptr);
 
 // The memory of a cache: keys, values and their scales (empty without them).
 struct CacheRows {

@@ -762,3 +762,23 @@ def test_work_past_what_a_call_uses(work):
     out = torch.empty(3, 64, dtype=BF16, device=DEV)
     ops.ii_linear(out, at, w, work=arena)
     _close(out, *ops_ref.linear(x, w, BF16))
+
+
+def test_cache_read_into_one_buffer():
+    """k and v of one buffer, side by side in any place of an axis; not one over the other."""
+    h, d, t = 3, 64, 5
+    cache = ops.Cache.empty(2, h, 16, d)
+    slots = torch.arange(t, device=DEV) * 3
+    k, v = (_normal(_gen(i), t, h, d) for i in (1, 2))
+    ops.ii_cache_write(cache, k, v, slots)
+    for n in (t, 1):
+        for shape, pick in (((2, n, h, d), lambda b: (b[0], b[1])), ((n, 2, h, d), lambda b: (b[:, 0], b[:, 1])),
+                            ((n, h, 2, d), lambda b: (b[:, :, 0], b[:, :, 1])),
+                            ((h, n, 2, d), lambda b: (b[:, :, 0].transpose(0, 1), b[:, :, 1].transpose(0, 1)))):
+            kb, vb = pick(torch.zeros(shape, dtype=BF16, device=DEV))
+            ops.ii_cache_read(cache, slots[:n], kb, vb)
+            assert torch.equal(kb.double(), ops_ref.kept(k[:n])[0])
+            assert torch.equal(vb.double(), ops_ref.kept(v[:n])[0])
+            with pytest.raises(ii.IIError) as e:
+                ops.ii_cache_read(cache, slots[:n], kb, kb)
+            assert e.value.name == "II_EOVERLAP"
