@@ -481,6 +481,9 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
     if (a.columns < 0 || a.columns > ((int64_t)1 << 40) / c.page || a.pages_stride < 0)
         return fail(II_EINVAL, "%s: a page table of %lld columns, stride %lld", fn,
                     (long long)a.columns, (long long)a.pages_stride);
+    uint64_t pages_stride;
+    if (__builtin_mul_overflow((uint64_t)(a.seqs > 1 ? a.pages_stride : 0), (uint64_t)4, &pages_stride))
+        return fail(II_EOVERFLOW, "%s: the stride of pages", fn);
     if (!std::isfinite(a.scale)) return fail(II_EINVAL, "%s: scale is not finite", fn);
     if (!a.q_start && a.rows != a.seqs)
         return fail(II_EINVAL, "%s: %lld rows for %lld sequences without q_start", fn,
@@ -491,8 +494,8 @@ int run(const ii_attend_args& a, const ii_cache& c, hipStream_t stream) {
                           a.out_head_stride, 2, true, &out)) ||
         (rc = check_heads(fn, "q", a.q, a.rows, a.heads, c.dim, a.q_row_stride, a.q_head_stride, 2,
                           false, &q)) ||
-        (rc = check_rows(fn, "pages", a.pages, a.seqs, (uint64_t)a.columns * 4,
-                         a.seqs > 1 ? (uint64_t)a.pages_stride * 4 : 0, 4, &table)) ||
+        (rc = check_rows(fn, "pages", a.pages, a.seqs, (uint64_t)a.columns * 4, pages_stride, 4,
+                         &table)) ||
         (rc = check_rows(fn, "lengths", a.lengths, 1, (uint64_t)a.seqs * 4, 0, 4, &lengths)) ||
         (rc = check_rows(fn, "q_start", a.q_start, a.q_start ? 1 : 0, ((uint64_t)a.seqs + 1) * 4, 0,
                          4, &starts)) ||

@@ -836,8 +836,10 @@ int check(const ii_linear_args& a) {
     const uint64_t m = a.m, n = a.n, k = a.k, size = 2, osize = a.out_dtype == II_F32 ? 4 : 2;
     static const char* const kResidual = "residual";
     Rows out, scratch, r;
-    int rc = check_rows(fn, "out", a.out, m, n * osize, (m > 1 ? a.out_stride : 0) * osize, osize,
-                        &out);
+    uint64_t out_stride;
+    if (__builtin_mul_overflow((uint64_t)(m > 1 ? a.out_stride : 0), osize, &out_stride))
+        return fail(II_EOVERFLOW, "%s: the stride of out", fn);
+    int rc = check_rows(fn, "out", a.out, m, n * osize, out_stride, osize, &out);
     if (rc || (rc = check_work(fn, a.work, a.work_bytes, &scratch)) ||
         (rc = check_apart(fn, "work", out, scratch)))
         return rc;

@@ -264,3 +264,13 @@ def test_keys_and_values_of_one_buffer(layout):
                     (c["k"] + 2 * a[1], "II_EOVERLAP"), (c["k"] + 2 * a[0], "II_EOVERLAP"),
                     (c["k"] + 2 * p * a[0], "II_EINVAL")):
         _refused(ops._call_write(ops._CACHE.pack(*{**c, "v": v}.values()), tokens, 0), name)
+
+
+@pytest.mark.parametrize("stride", [1 << 62, (1 << 62) + 32, 3 << 61])
+def test_strides_that_wrap(stride):
+    """Strides whose bytes pass 64 bits, where the wrapped ones would do."""
+    _refused(ops._call_linear(ops._LINEAR.pack(*{**LINEAR, "out_dtype": 7, "out_stride": stride}.values()), 0),
+             "II_EOVERFLOW")
+    cache = ops._CACHE.pack(*{**CACHE, "pages": 0}.values())
+    _refused(ops._call_attend(ops._ATTEND.pack(*{**ATTEND, "pages_stride": stride}.values()), cache, 0),
+             "II_EOVERFLOW")
