@@ -51,6 +51,13 @@ def _fits(ok, what: str) -> None:
         raise ValueError(what)
 
 
+def _code(names, key) -> int:
+    try:
+        return names[key]
+    except KeyError:
+        raise ValueError(f"{key} is none of {', '.join(map(str, names))}") from None
+
+
 def _rows(t, what: str) -> tuple[int, int]:
     """(address, row stride) of a matrix."""
     s, last = t.stride()
@@ -90,9 +97,9 @@ def ii_linear(out, x, w, *, bias=None, w2=None, bias2=None, residual=None, act: 
     if residual is not None:
         _fits(residual.shape == (m, n) and residual.dtype == dt, "residual is not [m, n] of x's type")
         rp, rs = _rows(residual, "residual")
-    args = _LINEAR.pack(_CODES[dt], _CODES[out.dtype], ACTS[act], 0, m, n, k, xp, xs, wp, ws, w2p,
-                        w2s, _vector(bias, n, dt, "bias"), _vector(bias2, n, dt, "bias2"), rp, rs,
-                        op, os_, *_work(work))
+    args = _LINEAR.pack(_code(_CODES, dt), _code(_CODES, out.dtype), _code(ACTS, act), 0, m, n, k, xp,
+                        xs, wp, ws, w2p, w2s, _vector(bias, n, dt, "bias"),
+                        _vector(bias2, n, dt, "bias2"), rp, rs, op, os_, *_work(work))
     rc = _call_linear(args, ii._stream(stream))
     if rc:
         ii._check(rc, "ii_linear")
@@ -112,7 +119,7 @@ class Cache:
               "k and v differ in shape, type or strides, or their last axis is not contiguous")
         ks = vs = sps = shs = sts = 0
         if k_scale is not None:
-            _fits(k_scale.shape == v_scale.shape == (*shape[:3], self.dim // 32)
+            _fits(v_scale is not None and k_scale.shape == v_scale.shape == (*shape[:3], self.dim // 32)
                   and k_scale.dtype == v_scale.dtype == torch.uint8
                   and k_scale.stride() == v_scale.stride() and k_scale.stride(3) == 1,
                   "scales are not uint8 [pages, heads, page, dim / 32] at the same strides")
@@ -121,7 +128,7 @@ class Cache:
         _fits((k.dtype == torch.float8_e4m3fn) == (k_scale is not None),
               "scales go with float8_e4m3fn, and only with it")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.args = _CACHE.pack(_CODES[k.dtype], self.heads, self.dim, self.page, pages,
+        self.args = _CACHE.pack(_code(_CODES, k.dtype), self.heads, self.dim, self.page, pages,
                                 k.data_ptr(), v.data_ptr(), ks, vs, ps, hs, ts, sps, shs, sts)
 
     @classmethod
@@ -142,7 +149,7 @@ def _tokens(cache: Cache, k, v, slots) -> bytes:
     ka, kb, kl = k.stride()
     va, vb, vl = v.stride()
     _fits(kl == vl == 1, "the last axis of k or v is not contiguous")
-    return _TOKENS.pack(_CODES[dt], 0, t, k.data_ptr(), ka, kb, v.data_ptr(), va, vb,
+    return _TOKENS.pack(_code(_CODES, dt), 0, t, k.data_ptr(), ka, kb, v.data_ptr(), va, vb,
                         slots.data_ptr())
 
 
@@ -182,7 +189,7 @@ def ii_attend(out, q, cache: Cache, pages, lengths, q_start=None, *, max_q: int 
     outr, outh, outl = out.stride()
     _fits(ql == outl == 1, "the last axis of q or out is not contiguous")
     at, table = _rows(pages, "pages")
-    args = _ATTEND.pack(_CODES[dt], heads, rows, seqs, q.data_ptr(), qr, qh, out.data_ptr(), outr,
+    args = _ATTEND.pack(_code(_CODES, dt), heads, rows, seqs, q.data_ptr(), qr, qh, out.data_ptr(), outr,
                         outh, at, table, columns, lengths.data_ptr(), starts, max_q, max_len,
                         window, dim ** -0.5 if scale is None else scale, 0, *_work(work))
     rc = _call_attend(args, cache.args, ii._stream(stream))

@@ -274,3 +274,20 @@ def test_strides_that_wrap(stride):
     cache = ops._CACHE.pack(*{**CACHE, "pages": 0}.values())
     _refused(ops._call_attend(ops._ATTEND.pack(*{**ATTEND, "pages_stride": stride}.values()), cache, 0),
              "II_EOVERFLOW")
+
+
+def test_types_and_activations_that_are_not_known():
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)  # noqa: E731
+    x, w, out = z(4, 64), z(32, 64), z(4, 32)
+    c64 = torch.complex64
+    scale = z(2, 1, 16, 2, dt=torch.uint8)
+    cache = ops.Cache(z(2, 1, 16, 64), z(2, 1, 16, 64))
+    slots, table, n = torch.arange(3), z(1, 2, dt=torch.int32), z(1, dt=torch.int32)
+    for call in (lambda: ops.ii_linear(out, x, w, act="tanh"),
+                 lambda: ops.ii_linear(out, x.to(c64), w.to(c64)), lambda: ops.ii_linear(out.to(c64), x, w),
+                 lambda: ops.Cache(z(2, 1, 16, 64, dt=c64), z(2, 1, 16, 64, dt=c64)),
+                 lambda: ops.Cache(*[z(2, 1, 16, 64, dt=torch.float8_e4m3fn)] * 2, scale),
+                 lambda: ops.ii_cache_write(cache, *[z(3, 1, 64, dt=c64)] * 2, slots),
+                 lambda: ops.ii_attend(*[z(1, 2, 64, dt=c64)] * 2, cache, table, n)):
+        with pytest.raises(ValueError):
+            call()
