@@ -35,7 +35,8 @@ __device__ inline float activate(float y, int act) {
     switch (act) {
     case II_ACT_RELU: return y < 0 ? 0.0f : y;  // NaN stays
     case II_ACT_SILU: return silu(y);
-    case II_ACT_GELU: return 0.5f * y * (1.0f + erff(y * 0.70710678118654752f));
+    // 1 + erf(x) = erfc(-x), which does not cancel where y is negative
+    case II_ACT_GELU: return 0.5f * y * erfcf(y * -0.70710678118654752f);
     }
     return y;
 }

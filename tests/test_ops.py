@@ -782,3 +782,16 @@ def test_cache_read_into_one_buffer():
             with pytest.raises(ii.IIError) as e:
                 ops.ii_cache_read(cache, slots[:n], kb, kb)
             assert e.value.name == "II_EOVERLAP"
+
+
+@pytest.mark.parametrize("m", [1, 3])       # 64 and 192 rows: small and large tiles
+def test_linear_gelu_of_negative_values(m):
+    """y from -10 to 10 through unit weights into f32, relative to the definition:
+    y / sqrt(2) is off by 2^-23 (its rounding and the constant's), which erfc turns
+    into at most y^2 + 1 times as much; erfc itself by 16 units, the products by 2."""
+    y = torch.linspace(-10, 10, 64 * 64 * m, device=DEV).to(BF16).view(-1, 64)
+    out = torch.empty(64 * m, 64, dtype=F32, device=DEV)
+    ops.ii_linear(out, y, torch.eye(64, dtype=BF16, device=DEV), act="gelu")
+    z = y.double().cpu()
+    want = 0.5 * z * torch.special.erfc(-z / math.sqrt(2))
+    _close(out.cpu(), want, want.abs() * (z * z + 19) * 2.0 ** -23)
