@@ -18,17 +18,23 @@ struct Linear {
     bool quads;  // four columns of out, biases and residual at a time
 };
 
-// y / (1 + exp(-y)). The exponent's product is kept in two parts, so that the
-// result is right to some units in the last place however negative y is; the
+// y / (1 + exp(-y)). The product of -y and log2(e) is kept in two floats (double-
+// length arithmetic), so that the exponential is right to some units in the last
+// place however negative y is. Below -64 both sides of the quotient are taken
+// 2^-64 times: 1 + exp(-y) passes float's range at -88 and its reciprocal leaves
+// the normal range at -87, where the quotient is normal down to -92. The
 // reciprocal is the hardware's (1 unit): the division took 5% of a large gated
 // product's time.
 __device__ inline float silu(float y) {
+#pragma clang fp contract(off)  // t is the rounded product everywhere
     constexpr float kHigh = -1.44269504f, kLow = -1.92596299e-8f;  // -log2(e)
-    // past 2^126 the quotient is below the normal range: 0, as at infinity
+    // at -200 the quotient is 0 already
     const float x = __builtin_amdgcn_fmed3f(y, -200.0f, 200.0f);
-    const float t = x * kHigh, rest = fmaf(x, kHigh, -t) + x * kLow;
-    const float e = __builtin_amdgcn_exp2f(t) * fmaf(rest, 0.693147181f, 1.0f);
-    return y * __builtin_amdgcn_rcpf(1.0f + e);
+    const float t = x * kHigh, rest = fmaf(x, kLow, fmaf(x, kHigh, -t));
+    const bool low = x < -64.0f;
+    const float s = low ? 0x1p-64f : 1.0f;
+    const float e = __builtin_amdgcn_exp2f(t - (low ? 64.0f : 0.0f)) * fmaf(rest, 0.693147181f, 1.0f);
+    return y * s * __builtin_amdgcn_rcpf(s + e);
 }
 
 __device__ inline float activate(float y, int act) {

@@ -795,3 +795,17 @@ def test_linear_gelu_of_negative_values(m):
     z = y.double().cpu()
     want = 0.5 * z * torch.special.erfc(-z / math.sqrt(2))
     _close(out.cpu(), want, want.abs() * (z * z + 19) * 2.0 ** -23)
+
+
+@pytest.mark.parametrize("m", [1, 3])
+@pytest.mark.parametrize("gated", [False, True])
+def test_linear_silu_of_negative_values(m, gated):
+    """y from -100 to 20 through unit weights into f32, relative to the definition:
+    8 units (ops_ref), half a unit of the least normal value where it ends below."""
+    y = torch.linspace(-100, 20, 64 * 64 * m, device=DEV).to(BF16).view(-1, 64)
+    out = torch.empty(64 * m, 64, dtype=F32, device=DEV)
+    eye = torch.eye(64, dtype=BF16, device=DEV)
+    ops.ii_linear(out, y, eye, w2=eye if gated else None, act="silu")
+    z = y.double().cpu()
+    want = z / (1 + torch.exp(-z)) * (z if gated else 1)
+    _close(out.cpu(), want, want.abs() * 2.0 ** -20 + 2.0 ** -127 * (z.abs() if gated else 1))
