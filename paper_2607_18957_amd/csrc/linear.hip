@@ -793,11 +793,12 @@ int run(const ii_linear_args& a, hipStream_t stream) {
     p.bias2 = static_cast<const T*>(a.bias2);
     p.residual = static_cast<const T*>(a.residual);
     p.out = a.out;
-    p.x_stride = a.x_stride;
-    p.w_stride = a.w_stride;
-    p.w2_stride = a.w2_stride;
-    p.residual_stride = a.residual_stride;
-    p.out_stride = a.out_stride;
+    // the stride of a single row says nothing of how it can be read
+    p.x_stride = a.m > 1 ? a.x_stride : 0;
+    p.w_stride = a.n > 1 ? a.w_stride : 0;
+    p.w2_stride = a.n > 1 ? a.w2_stride : 0;
+    p.residual_stride = a.m > 1 ? a.residual_stride : 0;
+    p.out_stride = a.m > 1 ? a.out_stride : 0;
     p.m = (int32_t)a.m;
     p.n = (int32_t)a.n;
     p.k = (int32_t)a.k;

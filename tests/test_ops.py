@@ -809,3 +809,18 @@ def test_linear_silu_of_negative_values(m, gated):
     z = y.double().cpu()
     want = z / (1 + torch.exp(-z)) * (z if gated else 1)
     _close(out.cpu(), want, want.abs() * 2.0 ** -20 + 2.0 ** -127 * (z.abs() if gated else 1))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 512, 9000), (1, 4096, 14336), (20, 1, 4096)])
+def test_linear_stride_of_a_single_row(m, n, k, work):
+    """The same kernel, so the same bits, whatever the stride of the only row is."""
+    g = _gen(14)
+    x, w = _normal(g, m, k), _normal(g, n, k, std=k ** -0.5)
+    r = _normal(g, m, n)
+    outs = []
+    for stride in (k, k + 1, 1, 1 << 40):
+        one = lambda t: t.as_strided(t.shape, (stride, 1)) if t.shape[0] == 1 else t  # noqa: E731
+        outs.append(torch.empty(m, n, dtype=F32, device=DEV))
+        ops.ii_linear(one(outs[-1]), one(x), one(w), residual=one(r), work=work)
+    _close(outs[0], *ops_ref.linear(x, w, F32, residual=r))
+    assert all(torch.equal(o, outs[0]) for o in outs)
