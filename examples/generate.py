@@ -114,6 +114,8 @@ def main() -> None:
     a.add_argument("--tokens", type=int, default=8)
     a.add_argument("--cache", choices=["fp8", "bf16"], default="fp8")
     a = a.parse_args()
+    if a.tokens < 1:
+        raise SystemExit("--tokens has to be 1 or more")
     table = getattr(synth, a.model)()
     plan, _arena, weights = load(table, normal_blob(table))
     prompts = [[(7 * i + j) % table.meta["vocab"] for j in range(n)] for i, n in enumerate((5, 37, 300))]

@@ -67,3 +67,15 @@ def test_generate(kept, most):
             p.append(int(row.argmax()))
         got = model.step(torch.tensor([p[-1] for p in prompts], device="cuda"), [1, 1, 1])
     plan.free()
+
+
+@pytest.mark.parametrize("count", ["0", "-300", "2"])
+def test_command_line(count, monkeypatch, capsys):
+    monkeypatch.setattr(sys, "argv", ["generate.py", "--tokens", count])
+    if int(count) < 1:
+        with pytest.raises(SystemExit) as e:
+            generate.main()
+        assert "1 or more" in str(e.value)
+    else:
+        generate.main()
+        assert capsys.readouterr().out.count("prompt of") == 3
