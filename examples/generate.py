@@ -59,6 +59,7 @@ class Model:
         # any order of pages will do
         self.pages = torch.randperm(seqs * columns, device="cuda").to(torch.int32).view(seqs, columns)
         self.lengths = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+        self.held = [0] * seqs      # the same on the host, to refuse what does not fit
         self.work = ops.work_buffer()
         angle = torch.arange(max_len, device="cuda")[:, None] * 10000.0 ** (
             -torch.arange(0, dim, 2, device="cuda") / dim)
@@ -80,6 +81,12 @@ class Model:
     def step(self, tokens, counts):
         """Logits of each sequence's last token after `counts` more tokens of
         each (a list of 1 or more), given one after another."""
+        held = [a + b for a, b in zip(self.held, counts)]
+        if len(counts) != len(self.held) or min(counts) < 1 or max(held) > self.max_len \
+                or sum(counts) != len(tokens):
+            raise ValueError(f"{counts} more tokens ({len(tokens)} given) after {self.held}, of up to "
+                             f"{self.max_len} each")
+        self.held = held
         stream = torch.cuda.current_stream()
         n = torch.tensor(counts, device="cuda")
         start = torch.zeros(len(counts) + 1, dtype=torch.int32, device="cuda")

@@ -69,6 +69,22 @@ def test_generate(kept, most):
     plan.free()
 
 
+def test_refuses_what_does_not_fit():
+    """Sequences past max_len, and counts that do not fit the tokens, are refused
+    before anything is launched; the model goes on as if they had not been given."""
+    table = synth.tiny()
+    plan, _arena, w = generate.load(table, generate.normal_blob(table))
+    model = generate.Model(w, table.meta, 64, 2, 20, page=16)
+    model.step(torch.arange(15, device="cuda"), [5, 10])
+    for tokens, counts in ((27, [16, 11]), (18, [16, 2]), (12, [1, 11]), (2, [2, 0]), (1, [1]), (3, [1, 1]),
+                           (3, [1, 1, 1])):
+        with pytest.raises(ValueError):
+            model.step(torch.arange(tokens, device="cuda"), counts)
+    assert model.step(torch.arange(25, device="cuda"), [15, 10]).isfinite().all()
+    assert model.lengths.tolist() == [20, 20]
+    plan.free()
+
+
 @pytest.mark.parametrize("count", ["0", "-300", "2"])
 def test_command_line(count, monkeypatch, capsys):
     monkeypatch.setattr(sys, "argv", ["generate.py", "--tokens", count])
