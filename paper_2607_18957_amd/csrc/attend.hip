@@ -73,14 +73,17 @@ __device__ inline float sum4(float x) {
 // (query, head of the group) rows of a sequence and cache head over a part of
 // its keys; its waves take steps of 32 keys in turn, each with its own running
 // maximum and sum, and load the next step's keys and values while they work on
-// one. 48 sequences of up to 8192 keys, 8 heads, 8 bits: 94 us, 4.4 TB/s; 2 of
-// up to 131072 in bf16: 176 us, 4.9 TB/s. Waves join in LDS, parts in `work` by the last workgroup to arrive.
+// one. 48 sequences of up to 8192 keys, 8 heads, 8 bits: 92 us, 4.4 TB/s (the
+// vector units, which unpack the codes, are busy in 31% of the cycles); 2 of up
+// to 131072 in bf16: 175 us, 5.0 TB/s. Waves join in LDS, parts in `work` by the
+// last workgroup to arrive.
 constexpr int kRowsHere = 16, kFewWaves = 4;
 
-// The most rows of a sequence that are few. Measured, few against many, 8 heads,
-// 8 bits, 16 sequences of up to 2001 keys: 64 rows 40 us against 61, 80 rows 35
-// against 78, 128 rows 51 against 69; 64 of up to 1001: 66 against 80, 58
-// against 93, 115 against 97.
+// The most rows of a sequence that are few. Measured, all as few against all as
+// many, 8 heads, 8 bits, 16 sequences of up to 2001 keys and up to 64 rows 42 us
+// against 61, 80 rows 36 against 61, 128 rows 53 against 60; 64 of up to 1001: 67
+// against 77, 59 against 76, 115 against 79. Of up to 128 rows some are few, and
+// both kernels run, one after the other: 76 and 112.
 constexpr int kFewRows = 96;
 
 constexpr int kPartsMost = 96;

@@ -122,6 +122,7 @@ __device__ inline bool join(float* red, uint32_t* counters, float* partial) {
 // each row) in turn, gridDim.y workgroups share a long k. Waves join their
 // sums in LDS in the order of the waves; workgroups leave theirs in `work`,
 // and the last to arrive adds them in the order of their places.
+// Bound by memory: 1 x 14336 x 4096 24.2 us, 4.9 TB/s.
 constexpr int kUnit = 64;  // elements of k a wave takes at once
 
 template <class T, bool kGated, int kRows, int kTokens, int kWaves, int kAhead>
@@ -219,7 +220,8 @@ __global__ __launch_bounds__(kWaves * 64) void linear_stream(Linear<T> p, uint32
 // Some tokens: as above, but rows of x go through LDS, where the kRowWaves
 // waves of a k group share them; each wave owns 16 weight rows (with a gate 16
 // of w and 16 of w2), kKGroups groups of waves and gridDim.y workgroups share
-// k. Weights are requested two chunks ahead of their use, x one.
+// k. Weights are requested two chunks ahead of their use, x one. Bound by
+// memory: 24 x 4096 x 14336 with a residual 31 us, 3.8 TB/s.
 constexpr int kRowWaves = 2, kKGroups = 8;
 constexpr int kChunkPad = 8;         // LDS rows 16 bytes apart in banks
 
@@ -363,6 +365,11 @@ __global__ __launch_bounds__(kRowWaves * kKGroups * 64) void linear_shared(Linea
 // eight lanes of one LDS cycle, a row each, meet all banks. A workgroup goes
 // on to its next tile's first words before it writes a tile. Few tiles share k
 // among gridDim.y workgroups, which leave their sums in `partial`.
+//
+// Bound by the matrix instructions, which the barriers between the stages keep
+// from being fed without a pause: 4099 x 14336 x 4096 with a gate 822 us, 1171
+// TFLOP/s, matrix units busy in 58% of the cycles. 256 x 256 takes every
+// register, and 6 to 8 more in scratch.
 constexpr int kTileK = 64, kTileWaves = 8;
 
 // 16 bytes a lane from r at offset + step into LDS, the wave's 1024 in a row.
@@ -702,11 +709,11 @@ void shared_launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
 // us that the pair is expected to take: a step of 64 elements of k takes each
 // shape so long with a workgroup a compute unit; joining costs its start and
 // the reading of the parts by the workgroup that comes last, at 60 GB/s.
-// Measured: 128 x 4096 x 4096 by 64 x 128 in 4 parts 18.7 us (expected 18);
-// 256 x 4096 x 4096 the same in 2 parts 23.7 (24); 1024 x 4096 x 4096 by
-// 128 x 256 in 2 parts 48 (44), by 64 x 128 54 (68); 512 x 4096 x 14336 by
-// 128 x 256 in 4 parts 86 (74); 512 x 14336 x 4096 with a gate by 256 x 256
-// 114 (110), by 128 x 256 128 (138).
+// Measured: 128 x 4096 x 4096 by 64 x 128 in 4 parts 17.6 us (expected 18);
+// 256 x 4096 x 4096 the same in 2 parts 22.6 (24); 1024 x 4096 x 4096 by
+// 128 x 256 in 2 parts 45 (44), by 64 x 128 55 (68); 512 x 4096 x 14336 by
+// 128 x 256 in 4 parts 75 (74); 512 x 14336 x 4096 with a gate by 256 x 256
+// 116 (110), by 128 x 256 128 (138).
 struct Shape {
     int m, n;
     double step;
@@ -760,19 +767,25 @@ void launch(const Linear<T>& p, const Work& work, hipStream_t stream) {
     const bool wide = p.k > 0 && p.k % 8 == 0 && words(p.x, p.x_stride) && words(p.w, p.w_stride) &&
                       (!p.w2 || words(p.w2, p.w2_stride));
     // rows of x that the waves' own loads find in the caches: 1 x 4096 x 14336
-    // 25.0 us against 28.1 through LDS, 1 x 128256 x 4096 177 against 186; from
-    // 8 tokens on it is 29.2 against 27.4, 212 against 191
+    // 24.6 us against 27.5 through LDS, 1 x 14336 x 4096 24.2 against 31 in
+    // tiles, 1 x 128256 x 4096 184 against 172-179; from 8 tokens on it is 28.7
+    // against 28.0, 212 against 176
     // (its grid has a workgroup for each 16 rows; a dispatch counts 2^32 lanes)
     if (wide && p.m <= 4 && p.n <= 1 << 26) return stream_waves<T, kGated, kGated ? 2 : 1, 1, 4>(p, work, stream);
     // rows that waves share through LDS, where it takes all waves of the card
-    // to keep up with the memory and a tile's rows would be too few: 24 x 4096
-    // x 14336 31.4 us against 33.6 in tiles; 24 x 14336 x 4096 with a gate
-    // 52.6 against 46
+    // to keep up with the memory and a tile's rows would be too few: 24 x 1024
+    // x 8192 9.3 us against 13.7 in tiles, 24 x 4096 x 4096 13.4 against 15.4.
+    // Tiles of larger matrices are as fast or faster where scratch lets them
+    // share k (24 x 4096 x 14336 31 against 28.5, 24 x 8192 x 8192 with a gate
+    // 65 against 60) and slower without (51 against 102, 65 against 78)
     if (wide && p.m <= 32 && p.n <= kRowWaves * 16 * (int)kUnits) {
         if (p.m <= 16) return shared_launch<T, kGated, 1>(p, work, stream);
         return shared_launch<T, kGated, 2>(p, work, stream);
     }
     // a tile's rows are addressed in 32 bits (strides may be less than k)
+    // Rows that are not whole words, or further apart, go through registers: 24
+    // x 4096 x 14336 48 us against 31, 256 x 4096 x 4096 44 against 23, 1 x
+    // 14336 x 4096 46 against 24, 4099 x 14336 x 4096 909 against 417
     const bool near = std::max({p.x_stride, p.w_stride, p.w2_stride, (int64_t)p.k}) < (1 << 21);
     const Choice c = choose_tile(p.m, p.n, p.k, kGated, work, wide && near ? 3 : 2);
     if (!wide || !near)
