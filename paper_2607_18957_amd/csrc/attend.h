@@ -49,7 +49,7 @@ __device__ inline bool not_finite(typename Vec<T>::x8 v) {
 
 // What is added to the exponents of weights, in bits, sums and totals alike, so
 // that the largest weight is 2^15 where the running maximum may be `grow` bits
-// behind: f16 has 10 bits of a weight down to 2^-14 alone and loses it below
+// behind: f16 has 11 bits of a weight down to 2^-14 alone and loses it below
 // 2^-25, and 131072 keys 2^-26 of the largest make 1/512 of a result. bf16 has
 // float's range.
 //
