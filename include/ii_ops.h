@@ -1,6 +1,7 @@
 /*
  * ii_ops.h -- running a model on the weights a load left in HBM: products
- * with its matrices, its key/value cache, attention over that cache.
+ * with its matrices, its key/value cache, attention over that cache, norms at
+ * the borders of blocks, rotary positions, log-probabilities.
  *
  * Conventions, beside those of ii.h:
  *   - Every pointer is device memory (or pinned host memory that the device
@@ -198,6 +199,186 @@ typedef struct ii_attend_args {
 } ii_attend_args;
 
 int ii_attend(const ii_attend_args* args, const ii_cache* cache, hipStream_t stream);
+
+/* ---- norms ------------------------------------------------------------- */
+enum {
+    II_NORM_RMS = 0,  /* y / sqrt(mean y^2 + eps) */
+    II_NORM_LAYER = 1 /* (y - mean y) / sqrt(mean (y - mean y)^2 + eps) */
+};
+
+/*
+ * ii_norm -- what lies between two blocks of a decoder: the norm after one,
+ * its gate and scale, the residual stream, the norm before the next. With
+ * N(y; w, b) = norm(y) * (w + offset) + b over each row of n elements:
+ *
+ *   y      = x, or N(x; post_weight, post_bias) if post
+ *   sum[i] = scale * gate[i] * y[i] + residual[i]
+ *   out[i] = N(sum[i]; weight, bias)
+ *
+ * All of it is held in 32 bits, the norms' sums in 64; sum and out are each
+ * rounded once (out is of sum as it was before).
+ *
+ *   dtype         of x, gate, weights, biases and out: II_BF16 or II_F16.
+ *   stream_dtype  of residual and sum: dtype or II_F32.
+ *   m             rows, 0 to 2^31 - 1.
+ *   n             elements of a row, 0 to 32768.
+ *   gate, residual   NULL: factors of 1, terms of 0.
+ *   post_weight, post_bias (if post), weight, bias (if out)   n elements; NULL:
+ *                 factors of 1 (offset is not added), terms of 0.
+ *   sum, out      NULL: not wanted (one of them is). sum may be residual itself,
+ *                 and out x.
+ *   scale, eps, offset   finite; eps not negative.
+ * Rows whose addresses and strides are multiples of 16 bytes, with n a multiple
+ * of 8, are read in words of 16 bytes, others by the element.
+ * Errors: II_EINVAL, II_EALIGN (an address not a multiple of its element),
+ * II_EOVERFLOW, II_EOVERLAP, II_EHIP.
+ */
+typedef struct ii_norm_args {
+    int32_t dtype, stream_dtype, kind, post;
+    int64_t m, n;
+    const void* x;
+    int64_t x_stride;
+    const void* gate;
+    int64_t gate_stride;
+    const void* residual;
+    int64_t residual_stride;
+    const void* post_weight;
+    const void* post_bias;
+    const void* weight;
+    const void* bias;
+    void* sum;
+    int64_t sum_stride;
+    void* out;
+    int64_t out_stride;
+    float scale, eps, offset;
+    int32_t reserved; /* 0 */
+} ii_norm_args;
+
+int ii_norm(const ii_norm_args* args, hipStream_t stream);
+
+/* ---- rotary positions -------------------------------------------------- */
+enum {
+    II_ROTARY_HALF = 0,       /* pairs (i, i + rot_dim / 2) */
+    II_ROTARY_INTERLEAVED = 1 /* pairs (2 i, 2 i + 1) */
+};
+
+/*
+ * How heads are turned by their token's position: pair i, (a, b), of the first
+ * rot_dim elements becomes
+ *
+ *   magnitude * (a cos t - b sin t),  magnitude * (b cos t + a sin t),
+ *   t = position * freqs[i],
+ *
+ * the elements from rot_dim on stay. Angles, sines and products are held in 64
+ * bits, so that far positions keep their angle and every result is the
+ * definition's, rounded once.
+ *
+ *   positions  of each token; any, though past 2^31 the angle is right to
+ *              2^-22 only.
+ *   freqs      rot_dim / 2 frequencies in radians, at most 2^10 in magnitude
+ *              (ii_rotary_freqs).
+ *   rot_dim    even, 0 to the heads' dim.
+ *   magnitude  finite.
+ */
+typedef struct ii_rotary {
+    const int64_t* positions;
+    const double* freqs;
+    int32_t rot_dim, layout;
+    float magnitude;
+    int32_t reserved; /* 0 */
+} ii_rotary;
+
+/*
+ * Heads to be turned: x [tokens, heads, dim] into out, which may be x itself.
+ *   dtype  II_BF16 or II_F16.
+ *   dim    a multiple of 8, 8 to 512.
+ * Addresses and strides are multiples of 16 bytes.
+ */
+typedef struct ii_turn {
+    int32_t dtype, heads, dim, reserved; /* reserved: 0 */
+    int64_t tokens;
+    const void* x;
+    int64_t x_token_stride, x_head_stride;
+    void* out;
+    int64_t out_token_stride, out_head_stride;
+} ii_turn;
+
+/* ii_rotate -- turn heads by their tokens' positions. */
+int ii_rotate(const ii_turn* heads, const ii_rotary* rotary, hipStream_t stream);
+
+/*
+ * ii_cache_append -- put tokens into a cache as ii_cache_write does, their keys
+ * turned on the way, and turn the queries q of the same tokens (NULL: none;
+ * dtype, tokens and dim as the keys'). A key is turned and quantised without a
+ * rounding between. Tokens without a slot have their queries turned.
+ */
+int ii_cache_append(const ii_cache* cache, const ii_tokens* from, const ii_rotary* rotary,
+                    const ii_turn* q, hipStream_t stream);
+
+/*
+ * ii_rotary_freqs -- frequencies of rot_dim / 2 pairs, host memory:
+ *
+ *   f[i] = base^(-2 i / rot_dim),
+ *
+ * for contexts `factor` times longer than the `original` one divided by factor
+ * where a pair turns less than `low` times over the original context, kept where
+ * it turns more than `high` times, and in proportion between:
+ *
+ *   r = original * f / (2 pi),  g = min(max((r - low) / (high - low), 0), 1),
+ *   f' = g f + (1 - g) f / factor.
+ *
+ * With original = 0 every pair is divided by factor (1: nothing is).
+ *   rot_dim  even, 0 to 2^20; base and factor positive; high above low; finite.
+ * Host only. Errors: II_EINVAL.
+ */
+int ii_rotary_freqs(int32_t rot_dim, double base, double factor, double low, double high,
+                    int64_t original, double* freqs);
+
+/*
+ * ii_logprobs -- what a model answers with: from the logits of a row
+ * [rows, vocab], z = scale * logits,
+ *
+ *   log p[j]   = z[j] - log sum_i exp z[i]
+ *   logprob    = log p[target]
+ *   entropy    = -sum_j p[j] log p[j]
+ *   top_ids    the `top` tokens of the largest logits, largest first, equal ones
+ *              by their number; top_logprobs their log p
+ *
+ * Exponentials are held in 32 bits, their sums in 64; each result is rounded once.
+ *
+ *   dtype    of the logits: II_F32, II_BF16 or II_F16.
+ *   rows     0 to 2^31 - 1.
+ *   vocab    1 to 2^31 - 1.
+ *   top      0 to 64. Places past the vocabulary get token -1 and -infinity.
+ *   targets  of each row; tokens outside the vocabulary give a logprob of 0.
+ *   logprob, entropy, top_ids, top_logprobs   [rows] and [rows, top], packed;
+ *            NULL: not wanted (logprob goes with targets, top_ids and
+ *            top_logprobs with a top above 0).
+ *   scale    positive and finite.
+ * Logits of -infinity have p = 0 and add nothing. In a row of nothing else every
+ * log p is -infinity and the entropy 0. In a row that holds NaN or +infinity
+ * log-probabilities and entropy are NaN; tokens are still in order, NaN above
+ * all (magnitudes of scale * logits past 32 bits count as infinite).
+ * Errors: II_EINVAL, II_EALIGN, II_EOVERFLOW, II_EOVERLAP, II_EHIP.
+ */
+#define II_MAX_TOP 64
+typedef struct ii_logprobs_args {
+    int32_t dtype, top;
+    int64_t rows, vocab;
+    const void* logits;
+    int64_t logits_stride;
+    const int64_t* targets;
+    float* logprob;
+    float* entropy;
+    int64_t* top_ids;
+    float* top_logprobs;
+    float scale;
+    int32_t reserved; /* 0 */
+    void* work;
+    uint64_t work_bytes;
+} ii_logprobs_args;
+
+int ii_logprobs(const ii_logprobs_args* args, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -13,20 +13,11 @@
 // three quarters of the cycles), read in 20, 5.1 TB/s; kept as they are, 134 MB
 // moved by each, 42 us together (with inputs that the last pass left in caches;
 // in 8 bits 46).
+#include "cache_device.h"
 #include "ops.h"
-#include "ops_device.h"
 
 namespace ii {
 namespace {
-
-struct Cache {
-    uint8_t* at[2];  // keys, values; bytes
-    uint8_t* scale[2];
-    int64_t page_stride, head_stride, token_stride;  // bytes
-    int64_t scale_page_stride, scale_head_stride, scale_token_stride;
-    int64_t pages;
-    int32_t page_bits;
-};
 
 struct Tokens {
     uint8_t* at[2];
@@ -38,16 +29,8 @@ struct Tokens {
 
 constexpr int kThreads = 256;
 
-// Exponent (biased) of a block's scale from the bits of its largest finite
-// magnitude: amax = 1.f * 2^E fits 448 = 1.75 * 2^8 at 2^(E - 8), or needs
-// one more if f > 0.75.
-__device__ inline uint32_t scale_exponent(uint32_t amax) {
-    const int e = (int)(amax >> 23) - 8 + ((amax & 0x7fffff) > 0x600000);
-    return e < 1 ? 1 : e;  // at most 247
-}
-
 template <class T, bool kQuant, bool kWrite>
-__global__ __launch_bounds__(kThreads) void cache_move(Cache c, Tokens f) {
+__global__ __launch_bounds__(kThreads) void cache_move(CacheAt c, Tokens f) {
     using x8 = typename Vec<T>::x8;
     const int per_head = f.dim / 8;
     const int64_t per_token = (int64_t)per_head * f.heads;
@@ -80,36 +63,13 @@ __global__ __launch_bounds__(kThreads) void cache_move(Cache c, Tokens f) {
     if (kWrite) {
         x8 v = {};
         if (kept) v = *user;
-        uint32_t amax = 0;
         float x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            x[j] = (float)v[j];
-            const uint32_t b = __builtin_bit_cast(uint32_t, x[j]) & 0x7fffffff;
-            if (b < 0x7f800000 && b > amax) amax = b;
-        }
-        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
-        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
-        const uint32_t e = scale_exponent(amax);
-        const float inverse = __builtin_bit_cast(float, (254 - e) << 23);
-        // 2^8 times a code above 240 is past the largest f16
-        const float most = sizeof(T) == 2 && __is_same(T, _Float16) && e == 127 + 8 ? 240.0f : 448.0f;
-        uint32_t code[2] = {};
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            float y[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t b = __builtin_bit_cast(uint32_t, x[j + i]) & 0x7fffffff;
-                y[i] = b < 0x7f800000 ? fminf(fmaxf(x[j + i] * inverse, -most), most)
-                                      : __builtin_nanf("");
-            }
-            int& w = reinterpret_cast<int&>(code[j / 4]);
-            w = j % 4 ? __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], w, true)
-                      : __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], w, false);
-        }
+        for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+        uint32_t e;
+        const u32x2 code = quantise<T>(x, &e);
         if (kept) {
-            *reinterpret_cast<u32x2*>(c.at[kv] + at + part * 8) = u32x2{code[0], code[1]};
+            *reinterpret_cast<u32x2*>(c.at[kv] + at + part * 8) = code;
             if (part % 4 == 0) c.scale[kv][sat] = (uint8_t)e;
         }
     } else if (live) {
@@ -134,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void cache_move(Cache c, Tokens f) {
 }
 
 template <class T>
-void launch(const Cache& c, const Tokens& f, bool quant, bool write, hipStream_t stream) {
+void launch(const CacheAt& c, const Tokens& f, bool quant, bool write, hipStream_t stream) {
     // a dispatch counts its work-items in 32 bits
     const int64_t per_token = (int64_t)f.heads * (f.dim / 8);
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 31) / per_token);
@@ -159,69 +119,28 @@ int move(const char* fn, const ii_cache* ca, const ii_tokens* tk, bool write, hi
     if (!ca || !tk) return fail(II_EINVAL, "%s: an argument is NULL", fn);
     const ii_cache& c = *ca;
     const ii_tokens& f = *tk;
-    const Checks checks;
-    CacheRows held;
-    int rc = check_cache(fn, c, write, &held);
-    if (rc) return rc;
-    if (!half_type(f.dtype)) return fail(II_EINVAL, "%s: dtype %d", fn, f.dtype);
-    if (c.dtype != II_FP8_E4M3 && c.dtype != f.dtype)
-        return fail(II_EINVAL, "%s: a cache of type %d, tokens of type %d", fn, c.dtype, f.dtype);
-    if (f.reserved) return fail(II_EINVAL, "%s: reserved is %d", fn, f.reserved);
-    if (f.tokens < 0 || f.tokens > (int64_t)1 << 40)
-        return fail(II_EINVAL, "%s: %lld tokens", fn, (long long)f.tokens);
+    {
+        const Checks checks;
+        TokenRows r;
+        if (const int rc = check_move(fn, c, f, write, &r)) return rc;
+    }
     if (!f.tokens) return II_OK;
-    Rows slots, rows[2];
-    Nest nest[2];
-    rc = check_rows(fn, "slots", f.slots, 1, (uint64_t)f.tokens * 8, 0, 8, &slots);
-    if (rc) return rc;
-    const int64_t ts[2] = {f.k_token_stride, f.v_token_stride};
-    const int64_t hs[2] = {f.k_head_stride, f.v_head_stride};
-    void* const at[2] = {f.k, f.v};
-    const char* const what[2] = {"k", "v"};
-    for (int i = 0; i < 2; ++i) {
-        rc = check_heads(fn, what[i], at[i], f.tokens, c.heads, c.dim, ts[i], hs[i], 2, !write,
-                         &rows[i], &nest[i]);
-        if (rc) return rc;
-    }
-    for (int i = 0; i < 2; ++i) {
-        if (!write && (rc = check_apart(fn, "slots", rows[i], slots))) return rc;
-        for (const Rows& r : held.all) {
-            rc = write ? check_apart(fn, what[i], r, rows[i]) : check_apart(fn, "the cache", rows[i], r);
-            if (rc) return rc;
-        }
-    }
-    if (write)
-        for (const Rows& r : held.all)
-            if ((rc = check_apart(fn, "slots", r, slots))) return rc;
-    if (!write && nests_meet(nest[0], nest[1])) return fail(II_EOVERLAP, "%s: k and v meet", fn);
-    Cache d;
-    const int size = c.dtype == II_FP8_E4M3 ? 1 : 2;
-    d.at[0] = static_cast<uint8_t*>(c.k);
-    d.at[1] = static_cast<uint8_t*>(c.v);
-    d.scale[0] = c.k_scale;
-    d.scale[1] = c.v_scale;
-    d.page_stride = c.page_stride * size;
-    d.head_stride = c.head_stride * size;
-    d.token_stride = c.token_stride * size;
-    d.scale_page_stride = c.scale_page_stride;
-    d.scale_head_stride = c.scale_head_stride;
-    d.scale_token_stride = c.scale_token_stride;
-    d.pages = c.pages;
-    d.page_bits = __builtin_ctz(c.page);
+    const CacheAt d = cache_at(c);
     Tokens t;
     for (int i = 0; i < 2; ++i) {
-        t.at[i] = static_cast<uint8_t*>(at[i]);
-        t.token_stride[i] = ts[i] * 2;
-        t.head_stride[i] = hs[i] * 2;
+        t.at[i] = static_cast<uint8_t*>(i ? f.v : f.k);
+        t.token_stride[i] = (i ? f.v_token_stride : f.k_token_stride) * 2;
+        t.head_stride[i] = (i ? f.v_head_stride : f.k_head_stride) * 2;
     }
     t.slots = f.slots;
     t.tokens = f.tokens;
     t.heads = c.heads;
     t.dim = c.dim;
+    const bool quant = c.dtype == II_FP8_E4M3;
     if (f.dtype == II_BF16)
-        launch<__bf16>(d, t, size == 1, write, stream);
+        launch<__bf16>(d, t, quant, write, stream);
     else
-        launch<_Float16>(d, t, size == 1, write, stream);
+        launch<_Float16>(d, t, quant, write, stream);
     return launched(fn);
 }
 

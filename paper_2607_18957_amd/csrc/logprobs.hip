@@ -1,0 +1,465 @@
+// ii_logprobs: log-probabilities of given tokens, entropy and the likeliest
+// tokens, in one pass over the logits.
+//
+// Every thread keeps the running maximum m of its logits, s = sum e^(z - m) and
+// t = sum e^(z - m) (z - m); then log sum_j e^z_j = m + log s, and the entropy is
+// log s - t / s. Sums of a tile are added up in 64 bits: a vocabulary is a long
+// sum, and what it loses is in every result. A logit is kept as a key of 64 bits,
+// its order above and its token's complement below, so that no two are alike and
+// the order of arrival does not show.
+//
+// The likeliest tokens: of a tile's 256 largest keys, one a thread, the top-th is
+// a bound that `top` tokens reach, and at most `top` threads hold tokens that do.
+// Those go into a list in LDS; later tiles add what is above the list's top-th,
+// which few are. A list is cut to `top` by counting, for each, those above it.
+//
+// Bound by memory; for 16-bit logits the vector units are close behind.
+#include <algorithm>
+#include <cmath>
+
+#include "ops.h"
+#include "ops_device.h"
+
+namespace ii {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kList = 2048;       // keys a list holds
+constexpr int kPruned = 256;      // and how many beyond 3 top are put up with
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Logprobs {
+    const void* logits;
+    const int64_t* targets;
+    float *logprob, *entropy, *top_logprobs;
+    int64_t* top_ids;
+    int64_t stride, rows;  // elements
+    int32_t vocab, top, parts, part;  // part: elements of one
+    float scale;
+    uint32_t* counters;
+    float* partial;
+    uint32_t room;  // floats of a part in partial
+};
+
+// A sum of exponentials relative to m.
+struct Sums {
+    float m;
+    double s, t;
+};
+__device__ inline Sums no_sums() { return Sums{-INFINITY, 0, 0}; }
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The same relative to m; m is not below a.m. Without a finite logit there is
+// nothing to move.
+__device__ inline void move_to(Sums& a, float m, float scale) {
+    if (a.m != m) {
+        if (a.m == -INFINITY) {
+            a.t = 0;
+        } else {
+            const float d = a.m - m;
+            const double c = exp2_of(d * scale * kLog2e);
+            a.t = c * (a.t + a.s * fmaxf(d, -3e38f));
+            a.s *= c;
+        }
+        a.m = m;
+    }
+}
+__device__ inline void join(Sums& a, Sums b, float scale) {
+    const float m = fmaxf(a.m, b.m);
+    move_to(a, m, scale);
+    move_to(b, m, scale);
+    a.s += b.s;
+    a.t += b.t;
+}
+
+__device__ inline Sums shuffled(const Sums& a, int d) {
+    Sums b;
+    b.m = __shfl_xor(a.m, d);
+    b.s = __shfl_xor(a.s, d);
+    b.t = __shfl_xor(a.t, d);
+    return b;
+}
+
+// The order of floats in whole numbers (-0 as +0; NaN as -infinity), above the
+// complement of the token, so that of equal logits the lower token is larger.
+// No key is 0.
+__device__ inline uint64_t key_of(float x, int token) {
+    if (!(x == x)) x = -INFINITY;
+    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
+    const uint32_t order = b & 0x80000000u ? ~b : b | 0x80000000u;
+    return (uint64_t)order << 32 | (uint32_t)~token;
+}
+__device__ inline float logit_of(uint64_t key) {
+    const uint32_t order = (uint32_t)(key >> 32);
+    return __builtin_bit_cast(float, order & 0x80000000u ? order & 0x7fffffffu : ~order);
+}
+
+struct List {
+    uint64_t key[kList];
+    uint64_t sorted[II_MAX_TOP];
+    uint64_t best[kThreads], least;  // of a tile
+    uint32_t count, added[3], again;
+};
+
+// How many of the n keys are above mine. n is even, or key[n] is 0.
+__device__ inline int above(const uint64_t* key, int n, uint64_t mine) {
+    using u64x2 = __attribute__((ext_vector_type(2))) uint64_t;
+    int c = 0;
+#pragma unroll 4
+    for (int i = 0; i < (n + 1) / 2; ++i) {
+        const u64x2 k = reinterpret_cast<const u64x2*>(key)[i];
+        c += (k[0] > mine) + (k[1] > mine);
+    }
+    return c;
+}
+
+// Cuts the list to its `top` largest keys, in order. Called by all threads with
+// what was written before them in place; they may read the list after it. Keys
+// of 0, which may be many, come last.
+__device__ inline void prune(List& l, int top) {
+    const int n = (int)l.count;
+    if (threadIdx.x < II_MAX_TOP) l.sorted[threadIdx.x] = 0;
+    if (threadIdx.x == 0 && n % 2) l.key[n] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const uint64_t mine = l.key[i];
+        const int c = above(l.key, n, mine);
+        if (c < top) l.sorted[c] = mine;
+    }
+    __syncthreads();
+    const int left = min(n, top);
+    if ((int)threadIdx.x < left) l.key[threadIdx.x] = l.sorted[threadIdx.x];
+    if (threadIdx.x == 0) l.count = left;
+    __syncthreads();
+}
+
+template <class T>
+struct Word {  // 16 bytes of logits
+    static constexpr int size = 16 / sizeof(T);
+};
+
+template <class T, bool kTop>
+__global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
+    constexpr int kWord = Word<T>::size, kWords = 16 / kWord;  // 16 logits a thread and tile
+    constexpr int kTile = kThreads * 16;
+    static_assert(II_MAX_TOP * 16 + II_MAX_TOP < kList - 1);
+    using vec = __attribute__((ext_vector_type(kWord))) T;
+    __shared__ __attribute__((aligned(16))) char lds[kTop ? sizeof(List) : 16];
+    __shared__ Sums waves[kThreads / 64];
+    List& list = *reinterpret_cast<List*>(lds);
+    const int t = threadIdx.x;
+    const float to2 = p.scale * kLog2e;
+
+    for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
+        // Words are whole ones of memory: tokens before the row's first and past
+        // its last are left out of the word that they share with it.
+        const T* logits = static_cast<const T*>(p.logits) + row * p.stride;
+        const int lead = (int)(reinterpret_cast<uintptr_t>(logits) % 16 / sizeof(T));
+        const vec* from = reinterpret_cast<const vec*>(logits - lead);
+        const int64_t begin = (int64_t)blockIdx.x * p.part;
+        const int64_t end = min(begin + p.part, (int64_t)p.vocab + lead);
+        Sums sums = no_sums();
+        uint64_t bound = 0;
+        if (kTop) {
+            if (t == 0) list.count = list.added[0] = list.added[1] = list.added[2] = 0;
+            __syncthreads();
+        }
+        int turn = 0;  // of three counters: one in use, one read, one cleared
+        for (int64_t base = begin; base < end; base += kTile) {
+            float x[16];
+            const auto at = [&](int i) { return base + ((int64_t)(i / kWord) * kThreads + t) * kWord + i % kWord; };
+            const bool whole = base >= lead && base + kTile <= end;
+            if (whole) {
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) {
+                    const vec v = from[at(w * kWord) / kWord];
+#pragma unroll
+                    for (int j = 0; j < kWord; ++j) x[w * kWord + j] = (float)v[j];
+                }
+            } else {
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) {
+                    vec v = {};
+                    if (at(w * kWord) < end) v = from[at(w * kWord) / kWord];
+#pragma unroll
+                    for (int j = 0; j < kWord; ++j) {
+                        const int64_t e = at(w * kWord + j);
+                        x[w * kWord + j] = e >= lead && e < end ? (float)v[j] : -INFINITY;
+                    }
+                }
+            }
+            float most = x[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) most = fmaxf(most, x[i]);
+            move_to(sums, fmaxf(sums.m, most), p.scale);
+            const float ref = sums.m == -INFINITY ? 0.0f : sums.m;
+            float s = 0, below = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float d = x[i] - ref, e = exp2_of(d * to2);
+                s += e;
+                below = fmaf(e, fmaxf(d, -3e38f), below);
+            }
+            sums.s += s;
+            sums.t += below;
+            if constexpr (kTop) {
+                const int top = p.top;
+                // a token as good as the bound's comes after it and is not above it
+                const auto real = [&](int i) { return whole || (at(i) >= lead && at(i) < end); };
+                const bool full = (int)list.count >= top;
+                const float least = logit_of(bound);
+                int hits = 0;
+                if (!full || most > least)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        hits += real(i) && key_of(x[i], (int)(at(i) - lead)) > bound;
+                uint32_t place = 0;
+                if (hits) place = atomicAdd(&list.added[turn], (uint32_t)hits);
+                __syncthreads();
+                uint32_t added = list.added[turn];
+                turn = turn == 2 ? 0 : turn + 1;
+                if (t == 0) list.added[turn == 2 ? 0 : turn + 1] = 0;
+                const uint32_t held = list.count;
+                if (added) {  // alike in all threads
+                    if (added > 3 * (uint32_t)top + kPruned || held + added > kList - 2) {
+                        // too many: the tile's own bound, unless fewer than
+                        // `top` threads hold any
+                        uint64_t mine = 0;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (real(i)) mine = max(mine, key_of(x[i], (int)(at(i) - lead)));
+                        list.best[t] = mine;
+                        if (t == 0) {
+                            list.least = 0;
+                            list.again = 0;
+                        }
+                        __syncthreads();
+                        if (mine && above(list.best, kThreads, mine) == top - 1) list.least = mine;
+                        __syncthreads();
+                        if (list.least) bound = max(bound, list.least - 1);
+                        prune(list, top);
+                        hits = 0;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            hits += real(i) && key_of(x[i], (int)(at(i) - lead)) > bound;
+                        if (hits) place = atomicAdd(&list.again, (uint32_t)hits);
+                        __syncthreads();
+                        added = list.again;
+                    }
+                    place += list.count;
+                    if (hits)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const uint64_t k = key_of(x[i], (int)(at(i) - lead));
+                            if (real(i) && k > bound) list.key[place++] = k;
+                        }
+                    __syncthreads();
+                    if (t == 0) list.count += added;
+                    __syncthreads();
+                    if ((int)list.count > 3 * top + kPruned || (int)list.count - (int)added < top) {
+                        prune(list, top);
+                        if ((int)list.count >= top) bound = list.key[top - 1];
+                    }
+                }
+            }
+        }
+
+        // the sums of the workgroup, in the order of its waves
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            // both lanes of a pair join the lower one's to the upper one's
+            const Sums o = shuffled(sums, d);
+            Sums a = t & d ? o : sums;
+            join(a, t & d ? sums : o, p.scale);
+            sums = a;
+        }
+        if (t % 64 == 0) waves[t / 64] = sums;
+        __syncthreads();
+        sums = waves[0];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) join(sums, waves[w], p.scale);
+        if constexpr (kTop) {
+            if (p.parts == 1 || (int)list.count > p.top) prune(list, p.top);
+        }
+
+        if (p.parts > 1) {
+            // a part: m, s, t, then its keys
+            const Rsrc parts = buffer(p.partial + row * p.parts * p.room,
+                                      (int64_t)p.parts * p.room * 4);
+            const uint32_t mine = blockIdx.x * p.room * 4;
+            using f64x2 = __attribute__((ext_vector_type(2))) double;
+            if (t == 0) {
+                leave_part(parts, mine, f32x4{sums.m, 0, 0, 0});
+                leave_part(parts, mine + 16, __builtin_bit_cast(f32x4, f64x2{sums.s, sums.t}));
+            }
+            using u64x2 = __attribute__((ext_vector_type(2))) uint64_t;
+            if (kTop)
+                for (int i = t * 2; i < p.top; i += kThreads * 2) {
+                    const int n = (int)list.count;
+                    leave_part(parts, mine + 32 + i * 8,
+                               __builtin_bit_cast(f32x4, u64x2{i < n ? list.key[i] : 0,
+                                                               i + 1 < n ? list.key[i + 1] : 0}));
+                }
+            if (!arrive_last(&p.counters[row], p.parts)) continue;
+            sums = no_sums();
+            for (int q = 0; q < p.parts; ++q) {
+                const f32x4 m = take_part(parts, q * p.room * 4);
+                const f64x2 st = __builtin_bit_cast(f64x2, take_part(parts, q * p.room * 4 + 16));
+                Sums b;
+                b.m = m[0];
+                b.s = st[0];
+                b.t = st[1];
+                join(sums, b, p.scale);
+            }
+            if constexpr (kTop) {
+                // as many parts at once as the list has room for beside `top`
+                const int pairs = (p.top + 1) / 2, step = max(1, (kList - 2 - p.top) / (2 * pairs));
+                if (t == 0) list.count = 0;
+                __syncthreads();
+                for (int q0 = 0; q0 < p.parts; q0 += step) {
+                    const int n = min(step, p.parts - q0), held = (int)list.count;
+                    for (int i = t; i < n * pairs; i += kThreads) {
+                        const u64x2 k = __builtin_bit_cast(
+                            u64x2, take_part(parts, (q0 + i / pairs) * p.room * 4 + 32 + i % pairs * 16));
+                        list.key[held + i * 2] = k[0];
+                        list.key[held + i * 2 + 1] = k[1];
+                    }
+                    __syncthreads();
+                    if (t == 0) list.count = held + n * pairs * 2;
+                    __syncthreads();
+                    prune(list, p.top);
+                }
+            }
+        }
+
+        // nothing but -infinity: every log-probability is -infinity, the entropy 0
+        const bool none = sums.m == -INFINITY && sums.s == 0;
+        const double logs = none ? 0.0 : log(sums.s);
+        const auto result = [&](float x) {
+            return none ? -INFINITY : (float)(((double)x - sums.m) * p.scale - logs);
+        };
+        if (t == 0) {
+            if (p.logprob) {
+                const int64_t target = p.targets[row];
+                p.logprob[row] = target >= 0 && target < p.vocab ? result((float)logits[target]) : 0.0f;
+            }
+            if (p.entropy) {
+                const double h = none ? 0.0 : logs - p.scale * (sums.t / sums.s);
+                p.entropy[row] = h < 0 ? 0.0f : (float)h;
+            }
+        }
+        if constexpr (kTop) {
+            for (int i = t; i < p.top; i += kThreads) {
+                // places past the vocabulary, which parts leave as 0
+                const uint64_t k = i < (int)list.count ? list.key[i] : 0;
+                p.top_ids[row * p.top + i] = k ? (int64_t)(uint32_t)~(uint32_t)k : -1;
+                p.top_logprobs[row * p.top + i] = k ? result(logit_of(k)) : -INFINITY;
+            }
+        }
+        __syncthreads();  // what LDS holds of this row has been read
+    }
+}
+
+template <class T>
+int run(const ii_logprobs_args& a, hipStream_t stream) {
+    Logprobs p;
+    p.logits = a.logits;
+    p.targets = a.targets;
+    p.logprob = a.logprob;
+    p.entropy = a.entropy;
+    p.top_ids = a.top_ids;
+    p.top_logprobs = a.top_logprobs;
+    p.stride = a.rows > 1 ? a.logits_stride : 0;
+    p.rows = a.rows;
+    p.vocab = (int32_t)a.vocab;
+    p.top = a.top;
+    p.scale = a.scale;
+    p.room = (uint32_t)groups(8 + 2 * a.top, 4) * 4;
+    p.counters = nullptr;
+    p.partial = nullptr;
+    // few rows are cut into parts of a tile or more
+    constexpr int64_t kTile = kThreads * 16, kWanted = 1024;
+    int64_t parts = 1;
+    if (a.work_bytes > kWorkHead && a.rows <= (int64_t)kWorkCounters) {
+        p.counters = static_cast<uint32_t*>(a.work);
+        p.partial = reinterpret_cast<float*>(static_cast<char*>(a.work) + kWorkHead);
+        const int64_t floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
+        parts = std::min({groups(a.vocab, kTile), kWanted / a.rows, floats / (a.rows * p.room)});
+        if (a.top) parts = std::min<int64_t>(parts, 1024 / a.top);
+        parts = std::max<int64_t>(parts, 1);
+    }
+    // a row may begin inside a word
+    p.part = (int32_t)(groups(groups(a.vocab + 7, parts), kTile / 16) * (kTile / 16));
+    p.parts = (int32_t)groups(a.vocab + 7, p.part);
+    const dim3 grid(p.parts, (uint32_t)std::min<int64_t>(a.rows, 65535));
+    if (a.top)
+        logprobs_rows<T, true><<<grid, kThreads, 0, stream>>>(p);
+    else
+        logprobs_rows<T, false><<<grid, kThreads, 0, stream>>>(p);
+    return launched("ii_logprobs");
+}
+
+int check(const ii_logprobs_args& a) {
+    const char* fn = "ii_logprobs";
+    if (!half_type(a.dtype) && a.dtype != II_F32) return fail(II_EINVAL, "%s: dtype %d", fn, a.dtype);
+    if (a.top < 0 || a.top > II_MAX_TOP) return fail(II_EINVAL, "%s: top is %d", fn, a.top);
+    if (a.reserved) return fail(II_EINVAL, "%s: reserved is %d", fn, a.reserved);
+    if (a.rows < 0 || a.rows > INT32_MAX || a.vocab < 1 || a.vocab > INT32_MAX - 16384)
+        return fail(II_EINVAL, "%s: %lld rows of %lld logits", fn, (long long)a.rows,
+                    (long long)a.vocab);
+    if (!std::isfinite(a.scale) || !(a.scale > 0)) return fail(II_EINVAL, "%s: scale %g", fn, a.scale);
+    if (!a.targets != !a.logprob)
+        return fail(II_EINVAL, "%s: logprob and targets go together", fn);
+    if (!a.top_ids != !a.top || !a.top_logprobs != !a.top)
+        return fail(II_EINVAL, "%s: top_ids and top_logprobs go with a top above 0", fn);
+    if (!a.logprob && !a.entropy && !a.top)
+        return fail(II_EINVAL, "%s: nothing is wanted", fn);
+    if (a.logits_stride < 0) return fail(II_EINVAL, "%s: a stride is negative", fn);
+    if (!a.rows) return II_OK;
+    const uint64_t rows = a.rows, size = a.dtype == II_F32 ? 4 : 2;
+    uint64_t stride;
+    if (__builtin_mul_overflow((uint64_t)(rows > 1 ? a.logits_stride : 0), size, &stride))
+        return fail(II_EOVERFLOW, "%s: the stride of logits", fn);
+    Rows logits, targets, scratch, out[4];
+    const uint64_t top = a.top;
+    const struct {
+        const char* what;
+        const void* p;
+        uint64_t bytes, align;
+    } outs[4] = {{"logprob", a.logprob, rows * 4, 4},
+                 {"entropy", a.entropy, rows * 4, 4},
+                 {"top_ids", a.top_ids, rows * top * 8, 8},
+                 {"top_logprobs", a.top_logprobs, rows * top * 4, 4}};
+    int rc = check_rows(fn, "logits", a.logits, rows, (uint64_t)a.vocab * size, stride, size, &logits);
+    if (!rc && a.targets) rc = check_rows(fn, "targets", a.targets, 1, rows * 8, 0, 8, &targets);
+    if (!rc) rc = check_work(fn, a.work, a.work_bytes, &scratch);
+    if (rc || (rc = check_apart(fn, "logits", scratch, logits)) ||
+        (rc = check_apart(fn, "targets", scratch, targets)))
+        return rc;
+    for (int i = 0; i < 4; ++i) {
+        if (!outs[i].p) continue;
+        rc = check_rows(fn, outs[i].what, outs[i].p, 1, outs[i].bytes, 0, outs[i].align, &out[i]);
+        if (rc || (rc = check_apart(fn, "logits", out[i], logits)) ||
+            (rc = check_apart(fn, "targets", out[i], targets)) ||
+            (rc = check_apart(fn, "work", out[i], scratch)))
+            return rc;
+        for (int j = 0; j < i; ++j)
+            if ((rc = check_apart(fn, outs[j].what, out[i], out[j]))) return rc;
+    }
+    return II_OK;
+}
+
+}  // namespace
+}  // namespace ii
+
+extern "C" int ii_logprobs(const ii_logprobs_args* a, hipStream_t stream) {
+    if (!a) return ii::fail(II_EINVAL, "ii_logprobs: args is NULL");
+    {
+        const ii::Checks checks;
+        if (const int rc = ii::check(*a)) return rc;
+    }
+    if (!a->rows) return II_OK;
+    if (a->dtype == II_F32) return ii::run<float>(*a, stream);
+    return a->dtype == II_BF16 ? ii::run<__bf16>(*a, stream) : ii::run<_Float16>(*a, stream);
+}

@@ -175,6 +175,44 @@ int check_cache(const char* fn, const ii_cache& c, bool written, CacheRows* held
     return II_OK;
 }
 
+int check_move(const char* fn, const ii_cache& c, const ii_tokens& f, bool write, TokenRows* r) {
+    CacheRows& held = r->cache;
+    int rc = check_cache(fn, c, write, &held);
+    if (rc) return rc;
+    if (!half_type(f.dtype)) return fail(II_EINVAL, "%s: dtype %d", fn, f.dtype);
+    if (c.dtype != II_FP8_E4M3 && c.dtype != f.dtype)
+        return fail(II_EINVAL, "%s: a cache of type %d, tokens of type %d", fn, c.dtype, f.dtype);
+    if (f.reserved) return fail(II_EINVAL, "%s: reserved is %d", fn, f.reserved);
+    if (f.tokens < 0 || f.tokens > (int64_t)1 << 40)
+        return fail(II_EINVAL, "%s: %lld tokens", fn, (long long)f.tokens);
+    if (!f.tokens) return II_OK;
+    Rows &slots = r->slots, *rows = r->kv;
+    Nest nest[2];
+    rc = check_rows(fn, "slots", f.slots, 1, (uint64_t)f.tokens * 8, 0, 8, &slots);
+    if (rc) return rc;
+    const int64_t ts[2] = {f.k_token_stride, f.v_token_stride};
+    const int64_t hs[2] = {f.k_head_stride, f.v_head_stride};
+    void* const at[2] = {f.k, f.v};
+    const char* const what[2] = {"k", "v"};
+    for (int i = 0; i < 2; ++i) {
+        rc = check_heads(fn, what[i], at[i], f.tokens, c.heads, c.dim, ts[i], hs[i], 2, !write,
+                         &rows[i], &nest[i]);
+        if (rc) return rc;
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (!write && (rc = check_apart(fn, "slots", rows[i], slots))) return rc;
+        for (const Rows& r : held.all) {
+            rc = write ? check_apart(fn, what[i], r, rows[i]) : check_apart(fn, "the cache", rows[i], r);
+            if (rc) return rc;
+        }
+    }
+    if (write)
+        for (const Rows& r : held.all)
+            if ((rc = check_apart(fn, "slots", r, slots))) return rc;
+    if (!write && nests_meet(nest[0], nest[1])) return fail(II_EOVERLAP, "%s: k and v meet", fn);
+    return II_OK;
+}
+
 int check_work(const char* fn, const void* work, uint64_t bytes, Rows* r) {
     *r = Rows{};
     if (!work && !bytes) return II_OK;

@@ -1,4 +1,4 @@
-// Argument checks that the operators (linear.hip, cache.hip, attend.hip) share.
+// Argument checks that the operators share.
 #pragma once
 
 #include <hip/hip_runtime_api.h>
@@ -65,6 +65,13 @@ struct CacheRows {
     Rows all[4];
 };
 int check_cache(const char* fn, const ii_cache& c, bool written, CacheRows* held);
+
+// Tokens on their way into a cache (write) or out of it.
+struct TokenRows {
+    CacheRows cache;
+    Rows kv[2], slots;  // slots and kv are empty without tokens
+};
+int check_move(const char* fn, const ii_cache& c, const ii_tokens& f, bool write, TokenRows* r);
 
 // Groups of `size` that hold n things; in 64 bits, as n + size - 1 need not fit n's type.
 constexpr int64_t groups(int64_t n, int64_t size) { return (n + size - 1) / size; }

@@ -1,5 +1,6 @@
 """Python binding of the operators in libii.so (include/ii_ops.h): products
-with a model's matrices, its paged key/value cache, attention over that cache.
+with a model's matrices, its paged key/value cache, attention over that cache,
+norms at the borders of blocks, rotary positions, log-probabilities of tokens.
 
 As in ``ii``, every function has the name of the C entry point it calls and
 turns its arguments into addresses, sizes and strides; the library checks and
@@ -21,24 +22,35 @@ import torch
 
 from . import ii
 
-__all__ = ["Cache", "ii_attend", "ii_cache_read", "ii_cache_write", "ii_linear", "work_buffer",
-           "WORK_BYTES"]
+__all__ = ["Cache", "ii_attend", "ii_cache_append", "ii_cache_read", "ii_cache_write", "ii_linear",
+           "ii_logprobs", "ii_norm", "ii_rotary_freqs", "ii_rotate", "work_buffer", "MAX_TOP", "WORK_BYTES"]
 
 WORK_BYTES = 64 << 20
+MAX_TOP = 64
 ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+NORMS = {"rms": 0, "layer": 1}
+LAYOUTS = {"half": 0, "interleaved": 1}
 
 _c = ii._c
 _lib = ii._lib
-for _n, _k in (("ii_linear", 1), ("ii_cache_write", 2), ("ii_cache_read", 2), ("ii_attend", 2)):
+for _n, _k in (("ii_linear", 1), ("ii_cache_write", 2), ("ii_cache_read", 2), ("ii_attend", 2),
+               ("ii_norm", 1), ("ii_rotate", 2), ("ii_cache_append", 4), ("ii_logprobs", 1)):
     ii._sig(_n, _c.c_int, *[_c.c_char_p] * _k, _c.c_void_p)
 _call_linear, _call_attend = _lib.ii_linear, _lib.ii_attend
 _call_write, _call_read = _lib.ii_cache_write, _lib.ii_cache_read
+_call_norm, _call_rotate = _lib.ii_norm, _lib.ii_rotate
+_call_append, _call_logprobs = _lib.ii_cache_append, _lib.ii_logprobs
+ii._sig("ii_rotary_freqs", _c.c_int, _c.c_int32, *[_c.c_double] * 4, _c.c_int64, _c.POINTER(_c.c_double))
 
 _CODES = {getattr(torch, n): c for c, n in ii._TORCH_DTYPES.items()}
 _LINEAR = struct.Struct("=4i3qPqPqPqPPPqPqPQ".replace("P", "Q"))  # struct ii_linear_args
 _CACHE = struct.Struct("=4iq4Q6q")                                # struct ii_cache
 _TOKENS = struct.Struct("=2iqQ2qQ2qQ")                            # struct ii_tokens
 _ATTEND = struct.Struct("=2i2qQ2qQ2qQ2q2Q3qfiQQ")                 # struct ii_attend_args
+_NORM = struct.Struct("=4i2qQqQqQq4QQqQq3fi")                     # struct ii_norm_args
+_ROTARY = struct.Struct("=2Q2ifi")                                # struct ii_rotary
+_TURN = struct.Struct("=4iqQ2qQ2q")                               # struct ii_turn
+_LOGPROBS = struct.Struct("=2i2qQq5Qfi2Q")                        # struct ii_logprobs_args
 
 
 def work_buffer(nbytes: int = WORK_BYTES, device="cuda"):
@@ -195,3 +207,116 @@ def ii_attend(out, q, cache: Cache, pages, lengths, q_start=None, *, max_q: int 
     rc = _call_attend(args, cache.args, ii._stream(stream))
     if rc:
         ii._check(rc, "ii_attend")
+
+
+def ii_norm(out, x, weight=None, *, bias=None, post: bool = False, post_weight=None, post_bias=None,
+            gate=None, residual=None, sum=None, scale: float = 1.0, kind: str = "rms",
+            eps: float = 1e-5, offset: float = 0.0, stream=None) -> None:
+    """sum = scale * gate * y + residual, y = x or (post) x normalised; out = sum
+    normalised. A norm is of kind "rms" or "layer", times (weight + offset), plus
+    bias. out or sum may be None; sum may be residual, and out x."""
+    (m, n), dt = x.shape, x.dtype
+    xp, xs = _rows(x, "x")
+    stream_dt = next((t.dtype for t in (residual, sum) if t is not None), dt)
+    at = []
+    for t, want, what in ((gate, dt, "gate"), (residual, stream_dt, "residual"), (sum, stream_dt, "sum"),
+                          (out, dt, "out")):
+        if t is None:
+            at += [0, 0]
+            continue
+        _fits(t.shape == (m, n) and t.dtype == want, f"{what} is not [m, n] of its type")
+        at += _rows(t, what)
+    vectors = [_vector(t, n, dt, w) for t, w in ((post_weight, "post_weight"), (post_bias, "post_bias"),
+                                                 (weight, "weight"), (bias, "bias"))]
+    args = _NORM.pack(_code(_CODES, dt), _code(_CODES, stream_dt), _code(NORMS, kind), bool(post), m, n, xp,
+                      xs, *at[:4], *vectors, *at[4:], scale, eps, offset, 0)
+    rc = _call_norm(args, ii._stream(stream))
+    if rc:
+        ii._check(rc, "ii_norm")
+
+
+def ii_rotary_freqs(rot_dim: int, *, base: float = 10000.0, factor: float = 1.0, low: float = 1.0,
+                    high: float = 4.0, original: int = 0, device="cuda"):
+    """Radians a position of each of rot_dim / 2 pairs: base^(-2 i / rot_dim),
+    divided by factor where a pair turns less than `low` times over the
+    `original` context, kept where it turns more than `high` times, in proportion
+    between (original 0: all are divided)."""
+    freqs = torch.empty(max(rot_dim // 2, 0), dtype=torch.float64)
+    rc = _lib.ii_rotary_freqs(rot_dim, base, factor, low, high, original,
+                              _c.cast(freqs.data_ptr(), _c.POINTER(_c.c_double)))
+    if rc:
+        ii._check(rc, "ii_rotary_freqs")
+    return freqs.to(device)
+
+
+def _rotary(tokens: int, positions, freqs, layout: str, magnitude: float) -> bytes:
+    _fits(freqs.dim() == 1, "freqs is not a vector")
+    return _ROTARY.pack(_vector(positions, tokens, torch.int64, "positions"),
+                        _vector(freqs, freqs.shape[0], torch.float64, "freqs"), 2 * freqs.shape[0],
+                        _code(LAYOUTS, layout), magnitude, 0)
+
+
+def _turn(out, x) -> bytes:
+    tokens, heads, dim = x.shape
+    _fits(out.shape == x.shape and out.dtype == x.dtype, "out and x differ in shape or type")
+    xt, xh, xl = x.stride()
+    ot, oh, ol = out.stride()
+    _fits(xl == ol == 1, "the last axis of x or out is not contiguous")
+    return _TURN.pack(_code(_CODES, x.dtype), heads, dim, 0, tokens, x.data_ptr(), xt, xh, out.data_ptr(),
+                      ot, oh)
+
+
+def ii_rotate(out, x, positions, freqs, *, layout: str = "half", magnitude: float = 1.0,
+              stream=None) -> None:
+    """Turn heads x [tokens, heads, dim] by their tokens' positions [tokens] into
+    out, which may be x: pair i of the first 2 * len(freqs) elements by position *
+    freqs[i], pairs (i, i + len(freqs)) or, "interleaved", (2 i, 2 i + 1)."""
+    rc = _call_rotate(_turn(out, x), _rotary(x.shape[0], positions, freqs, layout, magnitude),
+                      ii._stream(stream))
+    if rc:
+        ii._check(rc, "ii_rotate")
+
+
+def ii_cache_append(cache: Cache, k, v, slots, positions, freqs, *, q=None, q_out=None,
+                    layout: str = "half", magnitude: float = 1.0, stream=None) -> None:
+    """ii_cache_write with the keys turned by their tokens' positions on the way;
+    queries q [tokens, heads, dim] of the same tokens are turned into q_out, which
+    may be q."""
+    _fits((q is None) == (q_out is None), "q and q_out go together")
+    turn = None
+    if q is not None:
+        _fits(q.shape[0] == k.shape[0] and q.shape[2] == cache.dim and q.dtype == k.dtype,
+              "q is not [tokens, heads, dim] of the keys' type")
+        turn = _turn(q_out, q)
+    rc = _call_append(cache.args, _tokens(cache, k, v, slots),
+                      _rotary(k.shape[0], positions, freqs, layout, magnitude), turn, ii._stream(stream))
+    if rc:
+        ii._check(rc, "ii_cache_append")
+
+
+def ii_logprobs(logits, *, targets=None, logprob=None, entropy=None, top_ids=None, top_logprobs=None,
+                scale: float = 1.0, work=None, stream=None) -> None:
+    """From logits [rows, vocab], times scale: log-probabilities of targets [rows]
+    into logprob [rows], the entropy of each row into entropy [rows], the largest
+    logits' tokens, equal ones in their order, into top_ids [rows, top] and their
+    log-probabilities into top_logprobs."""
+    rows, vocab = logits.shape
+    at, stride = _rows(logits, "logits")
+    f32, i64 = torch.float32, torch.int64
+    top = 0
+    _fits((top_ids is None) == (top_logprobs is None), "top_ids and top_logprobs go together")
+    _fits((targets is None) == (logprob is None), "targets and logprob go together")
+    ids = values = 0
+    if top_ids is not None:
+        top = top_ids.shape[1]
+        _fits(top_ids.shape == top_logprobs.shape == (rows, top) and top_ids.is_contiguous()
+              and top_logprobs.is_contiguous() and top_ids.dtype == i64 and top_logprobs.dtype == f32,
+              "top_ids and top_logprobs are not contiguous [rows, top] of int64 and float32")
+        if top:
+            ids, values = top_ids.data_ptr(), top_logprobs.data_ptr()
+    args = _LOGPROBS.pack(_code(_CODES, logits.dtype), top, rows, vocab, at, stride,
+                          _vector(targets, rows, i64, "targets"), _vector(logprob, rows, f32, "logprob"),
+                          _vector(entropy, rows, f32, "entropy"), ids, values, scale, 0, *_work(work))
+    rc = _call_logprobs(args, ii._stream(stream))
+    if rc:
+        ii._check(rc, "ii_logprobs")
