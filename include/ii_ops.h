@@ -1,7 +1,7 @@
 /*
  * ii_ops.h -- running a model on the weights a load left in HBM: products
  * with its matrices, its key/value cache, attention over that cache, norms at
- * the borders of blocks, rotary positions, log-probabilities.
+ * the borders of blocks, rotary positions, low-rank adapters, log-probabilities.
  *
  * Conventions, beside those of ii.h:
  *   - Every pointer is device memory (or pinned host memory that the device
@@ -379,6 +379,53 @@ typedef struct ii_logprobs_args {
 } ii_logprobs_args;
 
 int ii_logprobs(const ii_logprobs_args* args, hipStream_t stream);
+
+/*
+ * ii_adapt -- low-rank adapters of many requests beside a shared projection:
+ *
+ *   h[i]   = A_a x[i],  out[i] = base[i] + scales[a] * B_a h[i],  a = adapters[i].
+ *
+ * Rows whose adapter is negative or not below `count` get base alone. Products
+ * are summed in 32 bits, h goes into the second product with 16 bits or more
+ * (24 where out is II_F32); out is rounded once.
+ *
+ *   dtype       of x, a, b: II_BF16 or II_F16; base_dtype and out_dtype: dtype or
+ *               II_F32.
+ *   m, n, k     0 to 2^31 - 1.
+ *   rank        1 to 256; count: adapters, 0 to 2^31 - 1.
+ *   a           [count, rank, k]: row r of adapter c at c * a_stride +
+ *               r * a_row_stride.
+ *   b           [count, n, rank], alike.
+ *   adapters    [m]; scales [count], NULL: factors of 1.
+ *   ranks       [count], NULL: all are `rank`. Adapter c uses the first ranks[c]
+ *               rows of its A and columns of its B; what lies past them is not
+ *               used. (Values outside 0 .. rank are taken as the nearer of these.)
+ *   base        NULL: zeros. It may be out itself.
+ *   work        h of (rows of) a call is kept here; without it each workgroup
+ *               forms it again, which is slower.
+ * Errors: II_EINVAL, II_EALIGN, II_EOVERFLOW, II_EOVERLAP, II_EHIP.
+ */
+typedef struct ii_adapt_args {
+    int32_t dtype, out_dtype, base_dtype, rank;
+    int64_t m, n, k, count;
+    const void* x;
+    int64_t x_stride;
+    const void* a;
+    int64_t a_stride, a_row_stride;
+    const void* b;
+    int64_t b_stride, b_row_stride;
+    const int32_t* adapters;
+    const float* scales;
+    const int32_t* ranks;
+    const void* base;
+    int64_t base_stride;
+    void* out;
+    int64_t out_stride;
+    void* work;
+    uint64_t work_bytes;
+} ii_adapt_args;
+
+int ii_adapt(const ii_adapt_args* args, hipStream_t stream);
 
 #ifdef __cplusplus
 }

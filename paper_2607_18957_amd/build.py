@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libii.so")
 SOURCES = ["plan.cpp", "scatter.hip", "runtime.hip", "ops.cpp", "linear.hip", "cache.hip",
-           "attend.hip", "attend_many.hip", "norm.hip", "rotate.hip", "logprobs.hip"]
+           "attend.hip", "attend_many.hip", "norm.hip", "rotate.hip", "logprobs.hip",
+           "adapt.hip"]
 ARCH = os.environ.get("II_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [

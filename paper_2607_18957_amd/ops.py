@@ -1,6 +1,7 @@
 """Python binding of the operators in libii.so (include/ii_ops.h): products
 with a model's matrices, its paged key/value cache, attention over that cache,
-norms at the borders of blocks, rotary positions, log-probabilities of tokens.
+norms at the borders of blocks, rotary positions, low-rank adapters, log-probabilities
+of tokens.
 
 As in ``ii``, every function has the name of the C entry point it calls and
 turns its arguments into addresses, sizes and strides; the library checks and
@@ -22,8 +23,8 @@ import torch
 
 from . import ii
 
-__all__ = ["Cache", "ii_attend", "ii_cache_append", "ii_cache_read", "ii_cache_write", "ii_linear",
-           "ii_logprobs", "ii_norm", "ii_rotary_freqs", "ii_rotate", "work_buffer", "MAX_TOP", "WORK_BYTES"]
+__all__ = ["Cache", "ii_adapt", "ii_attend", "ii_cache_append", "ii_cache_read", "ii_cache_write",
+           "ii_linear", "ii_logprobs", "ii_norm", "ii_rotary_freqs", "ii_rotate", "work_buffer", "MAX_TOP", "WORK_BYTES"]
 
 WORK_BYTES = 64 << 20
 MAX_TOP = 64
@@ -34,12 +35,14 @@ LAYOUTS = {"half": 0, "interleaved": 1}
 _c = ii._c
 _lib = ii._lib
 for _n, _k in (("ii_linear", 1), ("ii_cache_write", 2), ("ii_cache_read", 2), ("ii_attend", 2),
-               ("ii_norm", 1), ("ii_rotate", 2), ("ii_cache_append", 4), ("ii_logprobs", 1)):
+               ("ii_norm", 1), ("ii_rotate", 2), ("ii_cache_append", 4), ("ii_logprobs", 1),
+               ("ii_adapt", 1)):
     ii._sig(_n, _c.c_int, *[_c.c_char_p] * _k, _c.c_void_p)
 _call_linear, _call_attend = _lib.ii_linear, _lib.ii_attend
 _call_write, _call_read = _lib.ii_cache_write, _lib.ii_cache_read
 _call_norm, _call_rotate = _lib.ii_norm, _lib.ii_rotate
 _call_append, _call_logprobs = _lib.ii_cache_append, _lib.ii_logprobs
+_call_adapt = _lib.ii_adapt
 ii._sig("ii_rotary_freqs", _c.c_int, _c.c_int32, *[_c.c_double] * 4, _c.c_int64, _c.POINTER(_c.c_double))
 
 _CODES = {getattr(torch, n): c for c, n in ii._TORCH_DTYPES.items()}
@@ -51,6 +54,7 @@ _NORM = struct.Struct("=4i2qQqQqQq4QQqQq3fi")                     # struct ii_no
 _ROTARY = struct.Struct("=2Q2ifi")                                # struct ii_rotary
 _TURN = struct.Struct("=4iqQ2qQ2q")                               # struct ii_turn
 _LOGPROBS = struct.Struct("=2i2qQq5Qfi2Q")                        # struct ii_logprobs_args
+_ADAPT = struct.Struct("=4i4qQqQ2qQ2q3QQqQqQQ")                  # struct ii_adapt_args
 
 
 def work_buffer(nbytes: int = WORK_BYTES, device="cuda"):
@@ -320,3 +324,34 @@ def ii_logprobs(logits, *, targets=None, logprob=None, entropy=None, top_ids=Non
     rc = _call_logprobs(args, ii._stream(stream))
     if rc:
         ii._check(rc, "ii_logprobs")
+
+
+def ii_adapt(out, x, a, b, adapters, *, scales=None, ranks=None, base=None, work=None,
+             stream=None) -> None:
+    """out = base + scales[c] * B_c (A_c x) for each row of x [m, k], c its adapter
+    in adapters [m] (int32; none where it is negative or past the last): a [count,
+    rank, k], b [count, n, rank], of which adapter c uses the first ranks[c] rows
+    and columns. base [m, n] may be out; either may be float32."""
+    (m, k), (count, rank, ka), dt = x.shape, a.shape, x.dtype
+    n = b.shape[1]
+    _fits(ka == k and b.shape == (count, n, rank) and a.dtype == b.dtype == dt and out.shape == (m, n),
+          "shapes or types of out, x, a, b differ")
+    ac, ar, al = a.stride()
+    bc, br, bl = b.stride()
+    _fits((al == 1 or k < 2) and (bl == 1 or rank < 2), "the last axis of a or b is not contiguous")
+    xp, xs = _rows(x, "x")
+    op, os_ = _rows(out, "out")
+    bp = bs = 0
+    base_dt = dt
+    if base is not None:
+        _fits(base.shape == (m, n), "base is not [m, n]")
+        bp, bs = _rows(base, "base")
+        base_dt = base.dtype
+    args = _ADAPT.pack(_code(_CODES, dt), _code(_CODES, out.dtype), _code(_CODES, base_dt), rank, m, n, k,
+                       count, xp, xs, a.data_ptr(), ac, ar, b.data_ptr(), bc, br,
+                       _vector(adapters, m, torch.int32, "adapters"),
+                       _vector(scales, count, torch.float32, "scales"),
+                       _vector(ranks, count, torch.int32, "ranks"), bp, bs, op, os_, *_work(work))
+    rc = _call_adapt(args, ii._stream(stream))
+    if rc:
+        ii._check(rc, "ii_adapt")

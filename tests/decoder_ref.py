@@ -114,3 +114,34 @@ def logprobs(logits, scale=1.0):
     spread = (e * d * d).sum(-1, keepdim=True) / s     # |d| falls on t once more
     far = off * (1 + 2 * mean) + 4 * E * spread
     return logp, off + torch.where(logp > -math.inf, logp.abs(), 0.0) * 2 * E, h[:, 0], (far + h.abs() * 2 * E)[:, 0]
+
+
+def adapt(x, a, b, adapters, scales=None, ranks=None, base=None, out_dtype=None):
+    """(result, bound of the error) in 64 bits.
+
+    Sums as those of ops_ref.linear: k / 32 + 40 roundings of 2 E of the sum of
+    magnitudes, rank / 8 + 40 for the second. h goes into it in parts that leave
+    out 2^-16 of it (bf16) or 2^-22 (f16, or three parts), then three roundings."""
+    count, rank, k = a.shape
+    dt = out_dtype or x.dtype
+    m, n = x.shape[0], b.shape[1]
+    y = torch.zeros(m, n, dtype=torch.float64, device=x.device)
+    far = torch.zeros_like(y)
+    left = 2.0 ** -16 if x.dtype == torch.bfloat16 and dt != torch.float32 else 2.0 ** -22
+    for c in range(count):
+        rows = adapters == c
+        r = rank if ranks is None else min(max(int(ranks[c]), 0), rank)
+        if not rows.any() or not r:
+            continue
+        xc, ac, bc = x[rows].double(), a[c, :r].double(), b[c, :, :r].double()
+        h, size = xc @ ac.t(), xc.abs() @ ac.abs().t()
+        off = (k / 32 + 40) * 2 * E * size + left * h.abs()
+        if x.dtype == torch.float16:    # the parts of small ones beside the row's largest
+            off = off + 2.0 ** -36 * h.abs().amax(1, keepdim=True)
+        s = 1.0 if scales is None else scales[c].double()
+        y[rows] = s * (h @ bc.t())
+        far[rows] = abs(s) * ((off + (rank / 8 + 40) * 2 * E * (h.abs() + off)) @ bc.abs().t())
+    if base is not None:
+        y = y + base.double()
+    far = far + (y.abs() + (0 if base is None else base.double().abs())) * 4 * E
+    return y, far + (y.abs() + far) * U[dt] + TINY[dt]

@@ -1,0 +1,234 @@
+"""ii_adapt against its definition in 64 bits (decoder_ref), on the GPU: sizes,
+ranks and orders of adapters where it can go wrong."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # collected on CPU machines, never run there
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_2607_18957_amd import ii, ops  # noqa: E402  (fails loudly if libii.so is missing)
+
+import decoder_ref as ref  # noqa: E402
+
+DEV = torch.device("cuda:0")
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+NAN, INF = math.nan, math.inf
+
+
+@pytest.fixture(scope="module")
+def work():
+    return ops.work_buffer()
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _normal(g, *shape, dtype=BF16, std=1.0, pad=0, lead=0):
+    row = math.prod(shape[1:])
+    buf = torch.empty(shape[0] * (row + pad) + lead, device=DEV).normal_(0, std, generator=g).to(dtype)
+    return buf[lead:].view(shape[0], row + pad)[:, :row].unflatten(1, shape[1:])
+
+
+def _close(got, want, bound, what=""):
+    got = got.double()
+    same = (got == want) | (got.isnan() & want.isnan())
+    bad = ~(((got - want).abs() <= bound) | same)
+    if bad.any():
+        at = tuple(bad.nonzero()[0].tolist())
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} past the bound, first at {at}: "
+                             f"{got[at].item()} against {want[at].item()} +- {bound[at].item()}")
+
+
+def _ids(g, m, count, run=1):
+    """Adapters in runs, -1 and numbers past the last among them."""
+    ids = torch.randint(-1, count + 1, (-(-m // run),), generator=g, device=DEV).repeat_interleave(run)
+    return ids[:m].to(torch.int32).contiguous()
+
+
+def _adapt(g, m, n, k, rank, count, dt=BF16, out=None, base="", ids=None, scaled=True, ranks=None, pad=0,
+           lead=0, work=None):
+    out_dt = out or dt
+    x = _normal(g, m, k, dtype=dt, pad=pad, lead=lead)
+    a = _normal(g, count * rank, k, dtype=dt, std=max(k, 1) ** -0.5, pad=pad, lead=lead).unflatten(0, (count, rank))
+    b = _normal(g, count * n, rank, dtype=dt, std=rank ** -0.5, pad=pad, lead=lead).unflatten(0, (count, n))
+    ids = _ids(g, m, count) if ids is None else ids
+    scales = _normal(g, 1, count, dtype=F32)[0].contiguous() if scaled else None
+    ranks = None if ranks is None else torch.tensor(ranks, dtype=torch.int32, device=DEV)
+    base_dt = {"": None, "same": dt, "f32": F32, "in place": out_dt}[base]
+    held = None if base_dt is None else _normal(g, m, n, dtype=base_dt, pad=pad, lead=lead)
+    want, far = ref.adapt(x, a, b, ids, scales, ranks, held, out_dt)
+    to = held if base == "in place" else torch.full((m, n + pad), NAN, dtype=out_dt, device=DEV)[:, :n]
+    ops.ii_adapt(to, x, a, b, ids, scales=scales, ranks=ranks, base=held, work=work)
+    _close(to, want, far, f"{m} x {n} x {k}, rank {rank} of {count}")
+    if not base:
+        assert (to[(ids < 0) | (ids >= count)] == 0).all()
+    return to
+
+
+@pytest.mark.parametrize("m", [1, 2, 15, 16, 17, 40, 250])
+@pytest.mark.parametrize("n,k", [(1, 8), (64, 64), (100, 200), (513, 1000), (4096, 512), (96, 8192)])
+@pytest.mark.parametrize("split", [False, True])
+def test_adapt_few_rows(m, n, k, split, work):
+    g = _gen(m * 10007 + n)
+    for dt, rank, count in ((BF16, 16, 3), (F16, 8, 40), (BF16, 64, 1), (F16, 33, 5)):
+        _adapt(g, m, n, k, rank, count, dt, base="same", work=work if split else None)
+
+
+@pytest.mark.parametrize("m", [1025, 1500, 3000])
+@pytest.mark.parametrize("n,k", [(72, 200), (1000, 136), (260, 2048)])
+@pytest.mark.parametrize("split", [False, True])
+def test_adapt_many_rows(m, n, k, split, work):
+    g = _gen(m * 10007 + n)
+    for dt, rank, count, run in ((BF16, 16, 3, 400), (F16, 64, 9, 70), (BF16, 128, 2, 5), (F16, 24, 4, 1)):
+        _adapt(g, m, n, k, rank, count, dt, base="f32", ids=_ids(g, m, count, run), work=work if split else None)
+
+
+@pytest.mark.parametrize("rank", [1, 2, 7, 8, 9, 16, 24, 31, 32, 40, 64, 65, 100, 128, 129, 200, 256])
+@pytest.mark.parametrize("m", [5, 1100])
+@pytest.mark.parametrize("split", [False, True])
+def test_adapt_ranks(rank, m, split, work):
+    g = _gen(rank)
+    for dt, out in ((BF16, None), (F16, None), (BF16, F32), (F16, F32)):
+        _adapt(g, m, 130, 328, rank, 3, dt, out, "same", work=work if split else None)
+        _adapt(g, m, 130, 328, rank, 4, dt, out, ranks=[rank, 0, max(1, rank // 2), rank + 7],
+               work=work if split else None)
+
+
+@pytest.mark.parametrize("m", [9, 1100])
+@pytest.mark.parametrize("n,k,rank", [(127, 333, 16), (64, 64, 5), (33, 63, 8)])
+@pytest.mark.parametrize("split", [False, True])
+def test_adapt_odd_rows(m, n, k, rank, split, work):
+    """Rows that are not whole words, from odd places, further apart."""
+    g = _gen(n)
+    w = work if split else None
+    for base, out in (("", None), ("f32", None), ("same", F32), ("in place", None), ("in place", F32)):
+        _adapt(g, m, n, k, rank, 3, out=out, base=base, work=w)
+        _adapt(g, m, n, k, rank, 3, out=out, base=base, pad=5, lead=1, work=w)
+        _adapt(g, m, n, k, rank, 3, F16, out=out, base=base, pad=8, scaled=False, work=w)
+
+
+@pytest.mark.parametrize("split", [False, True])
+def test_adapt_orders(split, work):
+    """All rows of one adapter, each of its own, none of any, in turn, in runs that end inside a tile."""
+    g = _gen(1)
+    for m in (70, 1090):
+        i = torch.arange(m, device=DEV, dtype=torch.int32)
+        for ids in (torch.zeros_like(i), torch.full_like(i, 6), torch.full_like(i, -1), torch.full_like(i, 7),
+                    i % 7, i % 2, i // 17 % 7, torch.where(i == 40, 3, 5).int(), torch.where(i < 64, 2, -5).int()):
+            _adapt(g, m, 96, 192, 16, 7, ids=ids, base="same", work=work if split else None)
+    m = 200
+    _adapt(g, m, 96, 192, 16, m, ids=torch.randperm(m, generator=g, device=DEV).int(), work=work if split else None)
+
+
+def test_adapt_few_columns_and_no_sums(work):
+    g = _gen(2)
+    for m, n, k in ((0, 8, 8), (3, 0, 8), (3, 8, 0), (1100, 8, 0), (1100, 1, 3)):
+        _adapt(g, m, n, k, 4, 2, base="same", work=work)
+    x, out = _normal(g, 3, 64), torch.full((3, 32), NAN, dtype=BF16, device=DEV)
+    none = torch.empty(0, 8, 64, dtype=BF16, device=DEV), torch.empty(0, 32, 8, dtype=BF16, device=DEV)
+    ops.ii_adapt(out, x, *none, torch.zeros(3, dtype=torch.int32, device=DEV), work=work)
+    assert (out == 0).all()
+
+
+@pytest.mark.parametrize("m", [40, 1100])
+@pytest.mark.parametrize("split", [False, True])
+def test_adapt_nothing_leaks(m, split, work):
+    """What is not finite in an adapter, past a rank, or in a row stays there."""
+    g = _gen(3)
+    n, k, rank, count = 80, 128, 32, 4
+    x, base = _normal(g, m, k), _normal(g, m, n)
+    a, b = _normal(g, count, rank, k, std=k ** -0.5), _normal(g, count, n, rank, std=rank ** -0.5)
+    ids = torch.randint(0, 3, (m,), generator=g, device=DEV).int()
+    ids[7] = -1
+    ranks = torch.tensor([32, 8, 20, 32], dtype=torch.int32, device=DEV)
+    want, far = ref.adapt(x, a, b, ids, None, ranks, base)
+    a[3], b[3] = NAN, INF                       # no row has it
+    a[1, 8:], b[1, :, 8:] = NAN, INF            # past its rank
+    a[2, 20:], b[2, :, 20:] = INF, NAN
+    out = torch.empty(m, n, dtype=BF16, device=DEV)
+    ops.ii_adapt(out, x, a, b, ids, ranks=ranks, base=base, work=work if split else None)
+    _close(out, want, far)
+    b[0] = INF
+    x[3] = NAN
+    ids[3] = 1
+    ops.ii_adapt(out, x, a, b, ids, ranks=ranks, base=base, work=work if split else None)
+    rest = ids != 0
+    rest[3] = False
+    _close(out[rest], want[rest], far[rest])
+    assert out[3].isnan().all() and not out[ids == 0].isfinite().any()
+
+
+def test_adapt_far_values(work):
+    """h past f16's range, and far below it."""
+    g = _gen(4)
+    for std in (1e-6, 1e-3, 30.0):
+        x, a = _normal(g, 6, 4096, dtype=F16, std=std), _normal(g, 2, 16, 4096, dtype=F16, std=std)
+        b = _normal(g, 2, 64, 16, dtype=F16, std=1.0)
+        ids = torch.tensor([0, 1, 0, 1, 1, 0], dtype=torch.int32, device=DEV)
+        s = torch.tensor([0.01 / std ** 2, 0.02 / std ** 2], device=DEV)
+        out = torch.empty(6, 64, dtype=F16, device=DEV)
+        ops.ii_adapt(out, x, a, b, ids, scales=s, work=work)
+        _close(out, *ref.adapt(x, a, b, ids, s), f"{std}")
+
+
+def test_adapt_broadcast_and_same_bits(work):
+    g = _gen(5)
+    x = _normal(g, 1, 512).expand(30, 512)
+    a, b = _normal(g, 1, 16, 512, std=512 ** -0.5).expand(3, 16, 512), _normal(g, 1, 200, 16, std=0.25).expand(3, 200, 16)
+    base = _normal(g, 1, 200).expand(30, 200)
+    ids = torch.arange(30, device=DEV, dtype=torch.int32) % 3
+    out = torch.empty(30, 200, dtype=BF16, device=DEV)
+    ops.ii_adapt(out, x, a, b, ids, base=base, work=work)
+    _close(out, *ref.adapt(x, a, b, ids, None, None, base))
+    assert (out == out[0]).all()
+    for _ in range(4):
+        again = torch.empty_like(out)
+        ops.ii_adapt(again, x, a, b, ids, base=base, work=work)
+        assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("nbytes", [0, 65536, 65536 + 64, 65536 + 16 * 4 * 200, 1 << 20])
+@pytest.mark.parametrize("m", [200, 2100])
+def test_adapt_scratch(nbytes, m):
+    """Any size of scratch will do; its counters are left at zero."""
+    scratch = torch.zeros(nbytes, dtype=torch.uint8, device=DEV) if nbytes else None
+    _adapt(_gen(6), m, 300, 4000, 16, 5, base="same", work=scratch)
+    assert scratch is None or not scratch[:65536].any()
+
+
+def test_refusals(work):
+    g = _gen(7)
+    x, a, b = _normal(g, 4, 64), _normal(g, 2, 8, 64), _normal(g, 2, 32, 8)
+    ids, s, r = torch.zeros(4, dtype=torch.int32, device=DEV), torch.ones(2, device=DEV), torch.ones(2, device=DEV).int()
+    out = torch.zeros(4, 32, dtype=BF16, device=DEV)
+
+    def refused(name, call):
+        with pytest.raises(ii.IIError) as e:
+            call()
+        assert e.value.name == name, e.value
+        torch.cuda.synchronize()
+        assert not out.any()
+
+    for bad in (dict(x=x.cpu()), dict(a=a.cpu()), dict(b=b.cpu()), dict(adapters=ids.cpu()), dict(scales=s.cpu()),
+                dict(ranks=r.cpu()), dict(base=out.cpu()), dict(work=torch.zeros(64, dtype=torch.uint8))):
+        refused("II_EINVAL", lambda: ops.ii_adapt(out, **{**dict(x=x, a=a, b=b, adapters=ids), **bad}))
+    refused("II_EINVAL", lambda: ops.ii_adapt(out, x, _normal(g, 1, 257, 64), _normal(g, 1, 32, 257), ids))
+    room = torch.zeros(1 << 18, dtype=torch.uint8, device=DEV)
+    for what, t in dict(x=x, a=a, b=b, adapters=ids, scales=s, ranks=r, base=_normal(g, 4, 32)).items():
+        t = t.contiguous()
+        held = room[512:512 + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+        held.copy_(t)
+        args = {**dict(x=x, a=a, b=b, adapters=ids, scales=s, ranks=r), what: held}
+        over = room[528:528 + 256].view(BF16).view(4, 32) if t.numel() * t.element_size() >= 32 else \
+            room[512:512 + 256].view(BF16).view(4, 32)
+        refused("II_EOVERLAP", lambda: ops.ii_adapt(over, **args))
+        refused("II_EOVERLAP", lambda: ops.ii_adapt(out, work=room, **args))
+        assert torch.equal(held, t)
+    refused("II_EOVERLAP", lambda: ops.ii_adapt(out, x, a, b, ids, base=torch.as_strided(out, (4, 32), (0, 1))))
+    refused("II_EOVERLAP", lambda: ops.ii_adapt(room.view(BF16)[:128].view(4, 32), x, a, b, ids, work=room))
