@@ -2,18 +2,22 @@
 // out[i] = base[i] + s_a B_a (A_a x[i]), a the adapter of row i.
 //
 // Rows of one adapter share what is read of it, so rows are taken in tiles of
-// one adapter. A few rows, in any order, are gathered: the workgroup of a row
-// looks whether the row is the first, the 17th, .. of its adapter, takes it and
-// the next 15 if so, and ends if not. Of many rows, which come in runs, a
-// workgroup takes 64 neighbours, with a pass for each adapter among them.
+// one adapter. A few rows, in any order, are gathered: a workgroup counts the
+// rows of each adapter and finds which of them its tile of 16 has. Of many rows,
+// which come in runs, a tile is 64 neighbours, with a pass for each adapter among
+// them.
 //
-// h = A x is a sum over k that the waves of a workgroup, and workgroups, share;
-// it is short, and is kept in 32 bits (in `work`, or LDS). For the product with
-// B, whose matrix instruction takes 16 bits, a row of h is cut into two or three
-// parts of T, the second what the first's rounding left out: 16 bits of bf16 and
-// 22 of f16 in two parts, more than a result of 16 bits shows, and all 24 in
-// three, for a result of 32. Parts lie behind one another as one longer sum.
-// f16 has little range: rows are brought to its middle by a power of two first.
+// h = A x is a sum over k that the waves of a workgroup, and workgroups, share.
+// For the product with B, whose matrix instruction takes 16 bits, a row of h is
+// cut into two or three parts of T, the second what the first's rounding left
+// out: 16 bits of bf16 and 22 of f16 in two parts, more than a result of 16 bits
+// shows, and all 24 in three, for a result of 32. Parts lie behind one another as
+// one longer sum. f16 has little range: rows are brought to its middle by a power
+// of two first.
+//
+// A first kernel leaves the parts and the tiles' rows in `work`, a second one
+// forms the columns of out, in waves that share nothing and never wait for one
+// another. Without `work` each workgroup of a tile's columns forms h again, in LDS.
 #include <algorithm>
 #include <type_traits>
 
@@ -25,6 +29,7 @@ namespace {
 
 constexpr int kMaxRank = 256;
 constexpr int kGathered = 1024;  // rows that are gathered
+constexpr int kCounted = 1024;   // adapters (and none) whose rows are counted
 constexpr int kUnit = 64;        // elements of k a wave takes at once
 
 template <class T>
@@ -38,10 +43,15 @@ struct Adapt {
     int32_t m, n, k, rank, count;
     int32_t rankp;        // rank in whole words of 8
     int32_t parts, wide;  // parts of h; elements of a row of parts in LDS
-    int32_t columns;      // of out, a workgroup
+    int32_t columns;      // of out, a workgroup's
     int32_t splits;       // workgroups that share k
     bool out_f32, base_f32, words, b_words, quads;
-    float* h;             // [splits][m][rankp]
+    uint32_t* counters;
+    float* partial;       // [tiles][splits][rows of a tile][rankp]
+    // what the first kernel leaves of each row of each tile
+    T* held;              // [wide]
+    float* factor;        // of a result
+    int32_t *row, *id;    // -1: none
 };
 
 template <class T>
@@ -54,46 +64,81 @@ __device__ inline int rank_of(const Adapt<T>& p, int a) {
     return p.ranks ? min(max(p.ranks[a], 0), p.rank) : p.rank;
 }
 
-// A tile's rows and their adapters; rows past `count` have none.
+// A tile's rows and their adapters, -1 for none; places past the last row have
+// row -1.
 template <int kTok>
 struct Tile {
     int row[kTok], id[kTok];
-    float factor[kTok], shrunk[kTok];  // of a result, of h before it is cut
-    int count;
+    float factor[kTok];  // of a result
 };
 
-// The tile that begins with row b, false if none does. Called by all threads.
+// The rows of tile t of the gathered ones, false if there is none. Called by all
+// threads.
 template <class T, int kTok>
-__device__ inline bool gather(const Adapt<T>& p, int b, Tile<kTok>& tile) {
+__device__ inline bool gather(const Adapt<T>& p, int t, Tile<kTok>& tile) {
+    __shared__ int rows[kCounted];
+    constexpr int kWords = kGathered / 64;
     const int lane = threadIdx.x % 64;
-    const int mine = adapter_of(p, b);
-    int id[kGathered / 64];
+    int id[kWords];
 #pragma unroll
-    for (int i = 0; i < kGathered / 64; ++i) {
+    for (int i = 0; i < kWords; ++i) {
         const int j = i * 64 + lane;
         id[i] = j < p.m ? adapter_of(p, j) : -2;
     }
-    int before = 0, found = 0;
+    int mine = -2, from = 0;  // the tile's adapter; its rows from this one on
+    if (p.count < kCounted) {
+        // tiles in the order of adapters, those without one first
+        for (int e = threadIdx.x; e <= p.count; e += blockDim.x) rows[e] = 0;
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kGathered / 64; ++i) {
+        for (int i = 0; i < kWords; ++i)
+            if (i % (blockDim.x / 64) == threadIdx.x / 64 && id[i] >= -1) atomicAdd(&rows[id[i] + 1], 1);
+        __syncthreads();
+        int before = 0;
+        for (int c0 = 0; c0 <= p.count && mine == -2; c0 += 64) {
+            const int tiles = c0 + lane <= p.count ? (rows[c0 + lane] + kTok - 1) / kTok : 0;
+            int to = tiles;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int v = __shfl_up(to, d);
+                if (lane >= d) to += v;
+            }
+            to += before;
+            const uint64_t here = __ballot(to - tiles <= t && t < to);
+            if (here) {
+                const int at = __builtin_ctzll(here);
+                mine = c0 + at - 1;
+                from = (t - __shfl(to - tiles, at)) * kTok;
+            }
+            before = __shfl(to, 63);
+        }
+        if (mine == -2) return false;
+    } else {
+        // too many adapters to count: the tile that begins with row t, if one does
+        mine = adapter_of(p, t);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const int past = min(max(t - i * 64, 0), 64);  // of this word, before t
+            const uint64_t low = past == 64 ? ~0ull : (1ull << past) - 1;
+            from += __popcll(__ballot(id[i] == mine) & low);
+        }
+        if (from % kTok) return false;
+    }
+    int found = 0;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
         const uint64_t same = __ballot(id[i] == mine);
-        const int past = min(max(b - i * 64, 0), 64);  // of this word, before b
-        const uint64_t low = past == 64 ? ~0ull : (1ull << past) - 1;
-        before += __popcll(same & low);
-        const uint64_t rest = same & ~low;
-        const int place = found + __popcll(rest & ((1ull << lane) - 1));
-        if (threadIdx.x < 64 && rest >> lane & 1 && place < kTok) {
+        const int place = found + __popcll(same & ((1ull << lane) - 1)) - from;
+        if (threadIdx.x < 64 && same >> lane & 1 && place >= 0 && place < kTok) {
             tile.row[place] = i * 64 + lane;
             tile.id[place] = mine;
         }
-        found += __popcll(rest);
+        found += __popcll(same);
     }
-    if (before % kTok) return false;
-    if (threadIdx.x < kTok && (int)threadIdx.x >= found) {
-        tile.row[threadIdx.x] = b;
+    if (threadIdx.x < kTok && (int)threadIdx.x >= found - from) {
+        tile.row[threadIdx.x] = -1;
         tile.id[threadIdx.x] = -1;
     }
-    if (threadIdx.x == 0) tile.count = min(found, kTok);
     __syncthreads();
     return true;
 }
@@ -101,13 +146,11 @@ __device__ inline bool gather(const Adapt<T>& p, int b, Tile<kTok>& tile) {
 // Rows b kTok .. as they come.
 template <class T, int kTok>
 __device__ inline void neighbours(const Adapt<T>& p, int b, Tile<kTok>& tile) {
-    const int64_t first = (int64_t)b * kTok;
     if (threadIdx.x < kTok) {
-        const int64_t i = min(first + threadIdx.x, (int64_t)p.m - 1);
-        tile.row[threadIdx.x] = (int)i;
-        tile.id[threadIdx.x] = first + threadIdx.x < p.m ? adapter_of(p, i) : -1;
+        const int64_t i = (int64_t)b * kTok + threadIdx.x;
+        tile.row[threadIdx.x] = i < p.m ? (int)i : -1;
+        tile.id[threadIdx.x] = i < p.m ? adapter_of(p, i) : -1;
     }
-    if (threadIdx.x == 0) tile.count = (int)min((int64_t)kTok, p.m - first);
     __syncthreads();
 }
 
@@ -147,7 +190,7 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
     for (int r = 0; r < kR; ++r)  // rows past the rank are left out below
         ap[r] = p.a + a * p.a_stride + min(r0 + r * 16 + row, max(rank - 1, 0)) * p.a_row + part * 8;
 #pragma unroll
-    for (int t = 0; t < kTT; ++t) xp[t] = p.x + tile.row[t * 16 + row] * p.x_stride + part * 8;
+    for (int t = 0; t < kTT; ++t) xp[t] = p.x + max(tile.row[t * 16 + row], 0) * p.x_stride + part * 8;
     f32x4 acc[kR][kTT] = {};
     const int units = (int)groups(p.k, kUnit), whole = p.words ? p.k / kUnit : 0;
     const int step = kWaves * p.splits;
@@ -172,26 +215,26 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
                 for (int t = 0; t < kTT; ++t) acc[r][t] = mfma16(av[h][r], xv[h][t], acc[r][t]);
     };
     if (rank > r0) {
-        for (; u + (kAhead - 1) * step < whole; u += kAhead * step) {
+        for (; u < whole; u += kAhead * step) {
             x8 av[kAhead][2][kR], xv[kAhead][2][kTT];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) take(u + i * step, av[i], xv[i]);
+            for (int i = 0; i < kAhead; ++i)
+                if (u + i * step < whole) take(u + i * step, av[i], xv[i]);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) multiply(av[i], xv[i]);
+            for (int i = 0; i < kAhead; ++i)
+                if (u + i * step < whole) multiply(av[i], xv[i]);
         }
+        // what is left, past the last whole unit
+        while (u - step >= whole) u -= step;
         for (; u < units; u += step) {
             x8 av[2][kR], xv[2][kTT];
-            if (u < whole) {
-                take(u, av, xv);
-            } else {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int64_t k = (int64_t)u * kUnit + h * 32, left = p.k - k - part * 8;
+            for (int h = 0; h < 2; ++h) {
+                const int64_t k = (int64_t)u * kUnit + h * 32, left = p.k - k - part * 8;
 #pragma unroll
-                    for (int r = 0; r < kR; ++r) av[h][r] = some(ap[r] + k, left, p.words);
+                for (int r = 0; r < kR; ++r) av[h][r] = some(ap[r] + k, left, p.words);
 #pragma unroll
-                    for (int t = 0; t < kTT; ++t) xv[h][t] = some(xp[t] + k, left, p.words);
-                }
+                for (int t = 0; t < kTT; ++t) xv[h][t] = some(xp[t] + k, left, p.words);
             }
             multiply(av, xv);
         }
@@ -218,13 +261,13 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
 template <class T, int kTok, int kThreads>
 __device__ inline void cut(const Adapt<T>& p, Tile<kTok>& tile, const float* h, T* parts) {
     constexpr int kLanes = std::min(64, kThreads / kTok);
-    if (threadIdx.x < kTok * kLanes) {
-        const int token = threadIdx.x / kLanes, id = tile.id[token];
+    const int token = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    if (token < kTok) {
+        const float* mine = h + token * p.rankp;
         float up = 1, down = 1;
         if constexpr (std::is_same_v<T, _Float16>) {
             float most = 0;
-            for (int r = threadIdx.x % kLanes; r < p.rankp; r += kLanes)
-                most = fmaxf(most, fabsf(h[token * p.rankp + r]));
+            for (int r = lane; r < p.rankp; r += kLanes) most = fmaxf(most, fabsf(mine[r]));
 #pragma unroll
             for (int d = 1; d < kLanes; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
             // the largest to 2^12 .. 2^13
@@ -234,204 +277,350 @@ __device__ inline void cut(const Adapt<T>& p, Tile<kTok>& tile, const float* h, 
                 down = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
             }
         }
-        if (threadIdx.x % kLanes == 0) {
-            tile.shrunk[token] = down;
-            tile.factor[token] = id < 0 ? 0.0f : up * (p.scales ? p.scales[id] : 1.0f);
+        const int id = tile.id[token];
+        if (lane == 0) tile.factor[token] = id < 0 ? 0.0f : up * (p.scales ? p.scales[id] : 1.0f);
+        T* to = parts + token * p.wide;
+        for (int r = lane; r < p.rankp; r += kLanes) {
+            float rest = mine[r] * down;
+            for (int q = 0; q < p.parts; ++q) {
+                const T v = (T)rest;
+                to[q * p.rankp + r] = v;
+                rest -= (float)v;
+                if (!(fabsf(rest) <= 3e38f)) rest = 0;  // of what is not finite nothing is left
+            }
         }
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < kTok * p.wide; e += kThreads) {
-        const int token = e / p.wide, i = e % p.wide, part = i / p.rankp;
-        float rest = part < p.parts ? h[token * p.rankp + i % p.rankp] * tile.shrunk[token] : 0.0f;
-        T v = (T)rest;
-        for (int q = 0; q < part; ++q) {
-            rest -= (float)v;
-            if (!(fabsf(rest) <= 3e38f)) rest = 0;  // of what is not finite nothing is left
-            v = (T)rest;
-        }
-        parts[e] = v;
+        for (int i = p.parts * p.rankp + lane; i < p.wide; i += kLanes) to[i] = (T)0.0f;
     }
     __syncthreads();
 }
 
+// Columns j .. j + 3 of a row of base as they lie there; of out.
 template <class T>
-__device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 y) {
-    using x4 = typename Vec<T>::x4;
+__device__ inline u32x4 base_of(const Adapt<T>& p, int64_t row, int64_t j) {
+    u32x4 v = {};
+    const int64_t at = row * p.base_stride + j;
     if (p.quads && j + 4 <= p.n) {
-        if (p.base && p.base_f32) {
-            y += *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.base) + row * p.base_stride + j);
-        } else if (p.base) {
-            const x4 v = *reinterpret_cast<const x4*>(static_cast<const T*>(p.base) + row * p.base_stride + j);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] += (float)v[r];
-        }
-        if (p.out_f32) {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + row * p.out_stride + j) = y;
-        } else {
-            x4 v;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = (T)y[r];
-            *reinterpret_cast<x4*>(static_cast<T*>(p.out) + row * p.out_stride + j) = v;
-        }
-        return;
+        if (p.base_f32) return *reinterpret_cast<const u32x4*>(static_cast<const float*>(p.base) + at);
+        const u32x2 half = *reinterpret_cast<const u32x2*>(static_cast<const T*>(p.base) + at);
+        return u32x4{half[0], half[1], 0, 0};
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         if (j + r >= p.n) break;
-        float v = y[r];
-        if (p.base)
-            v += p.base_f32 ? static_cast<const float*>(p.base)[row * p.base_stride + j + r]
-                            : (float)static_cast<const T*>(p.base)[row * p.base_stride + j + r];
-        if (p.out_f32)
-            static_cast<float*>(p.out)[row * p.out_stride + j + r] = v;
+        if (p.base_f32)
+            v[r] = static_cast<const uint32_t*>(p.base)[at + r];
         else
-            static_cast<T*>(p.out)[row * p.out_stride + j + r] = (T)v;
+            v[r / 2] |= (uint32_t)static_cast<const uint16_t*>(p.base)[at + r] << r % 2 * 16;
+    }
+    return v;
+}
+template <class T>
+__device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 y, u32x4 base) {
+    using x4 = typename Vec<T>::x4;
+    if (p.base && p.base_f32) {
+        y += __builtin_bit_cast(f32x4, base);
+    } else if (p.base) {
+        const x4 v = __builtin_bit_cast(x4, u32x2{base[0], base[1]});
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] += (float)v[r];
+    }
+    const int64_t at = row * p.out_stride + j;
+    const bool whole = p.quads && j + 4 <= p.n;
+    if (p.out_f32) {
+        float* out = static_cast<float*>(p.out) + at;
+        if (whole) {
+            *reinterpret_cast<f32x4*>(out) = y;
+            return;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (j + r < p.n) out[r] = y[r];
+    } else {
+        T* out = static_cast<T*>(p.out) + at;
+        x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = (T)y[r];
+        if (whole) {
+            *reinterpret_cast<x4*>(out) = v;
+            return;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (j + r < p.n) out[r] = v[r];
     }
 }
 
-// Columns first .. end of the tile's rows of out, kC * 16 at a time a wave.
-template <class T, int kTT, int kC, int kWaves>
-__device__ inline void expand(const Adapt<T>& p, const Tile<kTT * 16>& tile, const T* parts, int64_t first,
+// Columns first, first + step, .. below end, kC * 16 at a time, of the kTT * 16
+// rows of out that a wave has: of each 16, lane l has row l mod 16, of which
+// `rows`, `ids` and `factors` are told, and `parts` is h cut, [row][wide]. kFast:
+// rankp, if a row's parts are two and stay in registers (0: neither).
+template <class T, int kTT, int kC, int kFast>
+__device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const int (&ids)[kTT],
+                              const float (&factors)[kTT], const T* parts, int64_t first, int64_t step,
                               int64_t end) {
     using x8 = typename Vec<T>::x8;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
-    const int steps = p.wide / 32, held = p.parts * p.rankp;
-    for (int64_t n0 = first + wave * kC * 16; n0 < end; n0 += kWaves * kC * 16) {
+    const int lane = threadIdx.x % 64, row = lane % 16, part = lane / 16;
+    const int held = p.parts * p.rankp;
+    constexpr int kSteps = kFast ? kFast * 2 / 32 : 1;
+    x8 hv[kSteps][kTT];
+    if constexpr (kFast != 0)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int t = 0; t < kTT; ++t)
+                hv[s][t] = *reinterpret_cast<const x8*>(parts + (t * 16 + row) * p.wide + s * 32 + part * 8);
+    const auto next = [&](int a) {
+        int v = INT32_MAX;
+#pragma unroll
+        for (int t = 0; t < kTT; ++t)
+            if (ids[t] > a) v = min(v, ids[t]);
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2) v = min(v, __shfl_xor(v, d));
+        return __builtin_amdgcn_readfirstlane(v);
+    };
+    for (int64_t n0 = first; n0 < end; n0 += step) {
+        u32x4 base[kC][kTT];
+        if (p.base)
+#pragma unroll
+            for (int t = 0; t < kTT; ++t)
+#pragma unroll
+                for (int c = 0; c < kC; ++c) {
+                    base[c][t] = u32x4{};
+                    if (rows[t] >= 0) base[c][t] = base_of(p, rows[t], n0 + c * 16 + part * 4);
+                }
         f32x4 total[kC][kTT] = {};
-        for (int a = next_adapter(tile, -1); a != INT32_MAX; a = next_adapter(tile, a)) {
+        for (int a = next(-1); a != INT32_MAX; a = next(a)) {
             const int rank = rank_of(p, a);
             const T* b[kC];
 #pragma unroll
             for (int c = 0; c < kC; ++c)
                 b[c] = p.b + a * p.b_stride + min(n0 + c * 16 + row, (int64_t)p.n - 1) * p.b_row;
             f32x4 acc[kC][kTT] = {};
-            int col = part * 8;
-            while (col >= p.rankp) col -= p.rankp;
-            for (int s = 0; s < steps; ++s) {
-                const int at = s * 32 + part * 8;
-                x8 bv[kC], hv[kTT];
+            if constexpr (kFast == 16) {
+                // both parts in one instruction
+                const int col = part % 2 * 8;
+#pragma unroll
+                for (int c = 0; c < kC; ++c) {
+                    const x8 bv = some(b[c] + col, rank - col, p.b_words);
+#pragma unroll
+                    for (int t = 0; t < kTT; ++t) acc[c][t] = mfma16(bv, hv[0][t], acc[c][t]);
+                }
+            } else if constexpr (kFast != 0) {
+                x8 bv[kC][kSteps / 2];
 #pragma unroll
                 for (int c = 0; c < kC; ++c)
-                    bv[c] = some(b[c] + col, at < held ? rank - col : 0, p.b_words);
 #pragma unroll
-                for (int t = 0; t < kTT; ++t)
-                    hv[t] = *reinterpret_cast<const x8*>(parts + (t * 16 + row) * p.wide + at);
+                    for (int s = 0; s < kSteps / 2; ++s) {
+                        const int col = s * 32 + part * 8;
+                        bv[c][s] = some(b[c] + col, rank - col, p.b_words);
+                    }
 #pragma unroll
-                for (int c = 0; c < kC; ++c)
+                for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-                    for (int t = 0; t < kTT; ++t) acc[c][t] = mfma16(bv[c], hv[t], acc[c][t]);
-                col += 32;
+                    for (int c = 0; c < kC; ++c)
+#pragma unroll
+                        for (int t = 0; t < kTT; ++t)
+                            acc[c][t] = mfma16(bv[c][s % (kSteps / 2)], hv[s][t], acc[c][t]);
+            } else {
+                int col = part * 8;
                 while (col >= p.rankp) col -= p.rankp;
+                for (int at = part * 8; at < p.wide; at += 32) {
+                    x8 bv[kC], h[kTT];
+#pragma unroll
+                    for (int c = 0; c < kC; ++c)
+                        bv[c] = some(b[c] + col, at < held ? rank - col : 0, p.b_words);
+#pragma unroll
+                    for (int t = 0; t < kTT; ++t)
+                        h[t] = *reinterpret_cast<const x8*>(parts + (t * 16 + row) * p.wide + at);
+#pragma unroll
+                    for (int c = 0; c < kC; ++c)
+#pragma unroll
+                        for (int t = 0; t < kTT; ++t) acc[c][t] = mfma16(bv[c], h[t], acc[c][t]);
+                    col += 32;
+                    while (col >= p.rankp) col -= p.rankp;
+                }
             }
             // a row has one adapter; what others have there does not matter
 #pragma unroll
             for (int t = 0; t < kTT; ++t)
-                if (tile.id[t * 16 + row] == a)
+                if (ids[t] == a)
 #pragma unroll
-                    for (int c = 0; c < kC; ++c) total[c][t] = acc[c][t] * tile.factor[t * 16 + row];
+                    for (int c = 0; c < kC; ++c) total[c][t] = acc[c][t] * factors[t];
         }
 #pragma unroll
         for (int t = 0; t < kTT; ++t)
-            if (t * 16 + row < tile.count)
+            if (rows[t] >= 0)
 #pragma unroll
                 for (int c = 0; c < kC; ++c)
-                    put(p, tile.row[t * 16 + row], n0 + c * 16 + part * 4, total[c][t]);
+                    put(p, rows[t], n0 + c * 16 + part * 4, total[c][t], base[c][t]);
     }
 }
 
-enum { kBoth, kShrink, kExpand };
-
-// kBoth: h in LDS, formed by each of the workgroups that share a tile's columns.
-// kShrink: a share of k of h, into memory. kExpand: the rest.
-template <class T, int kStage, int kR, int kTT, int kWaves>
-__global__ __launch_bounds__(kWaves * 64) void adapt_tiles(Adapt<T> p) {
+// h of tile blockIdx.x, cut: in LDS, formed by each of the workgroups that share
+// the tile's columns, which follow (kBoth); or in memory, by the last to arrive of
+// those that share k.
+template <class T, bool kBoth, int kR, int kTT, int kWaves>
+__global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
     constexpr int kTok = kTT * 16, kThreads = kWaves * 64;
-    constexpr int kRed = kStage == kExpand ? 0 : kWaves * kR * kTT * 256;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Tile<kTok> tile;
+    const int64_t first = (int64_t)blockIdx.x * kTok;  // of the rows in memory
     if constexpr (kTT == 1) {
-        if (!gather(p, blockIdx.x, tile)) return;
+        if (!gather(p, blockIdx.x, tile)) {
+            if (!kBoth && blockIdx.y == 0 && threadIdx.x < kTok) p.row[first + threadIdx.x] = -1;
+            return;
+        }
     } else {
         neighbours(p, blockIdx.x, tile);
     }
     float* red = reinterpret_cast<float*>(lds);
-    float* h = red + kRed;
-    if constexpr (kStage != kExpand) {
-        if constexpr (kStage == kBoth)
-            for (int e = threadIdx.x; e < kTok * p.rankp; e += kThreads) h[e] = 0;
-        __syncthreads();
-        for (int a = next_adapter(tile, -1); a != INT32_MAX; a = next_adapter(tile, a))
-            for (int r0 = 0; r0 < p.rankp; r0 += kR * 16)
-                shrink<T, kR, kTT, kWaves>(
-                    p, tile, a, r0, kStage == kBoth ? 0 : blockIdx.y, red, [&](int token, int r, float v) {
-                        if (kStage == kBoth)
-                            h[token * p.rankp + r] = v;
-                        else
-                            p.h[((int64_t)blockIdx.y * p.m + tile.row[token]) * p.rankp + r] = v;
-                    });
-    } else {
-        for (int e = threadIdx.x; e < kTok * p.rankp; e += kThreads) {
-            const int token = e / p.rankp, r = e % p.rankp;
-            float v = 0;
-            if (tile.id[token] >= 0)
-                for (int s = 0; s < p.splits; ++s)
-                    v += p.h[((int64_t)s * p.m + tile.row[token]) * p.rankp + r];
-            h[e] = v;
-        }
-        __syncthreads();
-    }
-    if constexpr (kStage != kShrink) {
-        T* parts = reinterpret_cast<T*>(h + kTok * p.rankp);
+    float* h = red + kWaves * kR * kTT * 256;
+    const int sums = kTok * p.rankp;
+    for (int e = threadIdx.x; e < sums; e += kThreads) h[e] = 0;
+    __syncthreads();
+    for (int a = next_adapter(tile, -1); a != INT32_MAX; a = next_adapter(tile, a))
+        for (int r0 = 0; r0 < p.rankp; r0 += kR * 16)
+            shrink<T, kR, kTT, kWaves>(p, tile, a, r0, kBoth ? 0 : blockIdx.y, red,
+                                       [&](int token, int r, float v) { h[token * p.rankp + r] = v; });
+    if constexpr (kBoth) {
+        T* parts = reinterpret_cast<T*>(h + sums);
         cut<T, kTok, kThreads>(p, tile, h, parts);
-        const int64_t first = (int64_t)blockIdx.y * p.columns;
-        expand<T, kTT, kTT == 1 ? 4 : 2, kWaves>(p, tile, parts, first, min(first + p.columns, (int64_t)p.n));
+        const int row = threadIdx.x % 16;
+        int rows[kTT], ids[kTT];
+        float factors[kTT];
+#pragma unroll
+        for (int t = 0; t < kTT; ++t) {
+            rows[t] = tile.row[t * 16 + row];
+            ids[t] = tile.id[t * 16 + row];
+            factors[t] = tile.factor[t * 16 + row];
+        }
+        constexpr int kC = kTT == 1 ? 4 : 2;
+        const int64_t at = (int64_t)blockIdx.y * p.columns;
+        expand<T, kTT, kC, 0>(p, rows, ids, factors, parts, at + threadIdx.x / 64 * kC * 16,
+                              kWaves * kC * 16, min(at + p.columns, (int64_t)p.n));
+    } else {
+        if (p.splits > 1) {
+            const Rsrc parts = buffer(p.partial + (int64_t)blockIdx.x * p.splits * sums,
+                                      (int64_t)p.splits * sums * 4);
+            for (int e = threadIdx.x * 4; e < sums; e += kThreads * 4)
+                leave_part(parts, (blockIdx.y * sums + e) * 4, *reinterpret_cast<f32x4*>(h + e));
+            if (!arrive_last(&p.counters[blockIdx.x], p.splits)) return;
+            for (int e = threadIdx.x * 4; e < sums; e += kThreads * 4) {
+                f32x4 s = {};
+#pragma unroll 8
+                for (int y = 0; y < p.splits; ++y) s += take_part(parts, (y * sums + e) * 4);
+                *reinterpret_cast<f32x4*>(h + e) = s;
+            }
+            __syncthreads();
+        }
+        cut<T, kTok, kThreads>(p, tile, h, p.held + first * p.wide);
+        if (threadIdx.x < kTok) {
+            p.row[first + threadIdx.x] = tile.row[threadIdx.x];
+            p.id[first + threadIdx.x] = tile.id[threadIdx.x];
+            p.factor[first + threadIdx.x] = tile.factor[threadIdx.x];
+        }
     }
 }
 
-template <class T, int kStage, int kR, int kTT, int kWaves>
-void stage_launch(Adapt<T> p, uint32_t tiles, uint32_t shares, hipStream_t stream) {
-    constexpr int kTok = kTT * 16;
-    uint32_t lds = kStage == kExpand ? 0 : kWaves * kR * kTT * 1024;
-    if (kStage != kShrink) lds += kTok * (p.rankp * 4 + p.wide * 2);
+// Columns of tile blockIdx.x from what adapt_shrink left: of a workgroup's waves
+// kTok / (kTT * 16) share its rows, the others its columns.
+template <class T, int kTok, int kTT, int kC, int kFast, int kWaves>
+__global__ __launch_bounds__(kWaves * 64) void adapt_expand(Adapt<T> p) {
+    constexpr int kSides = kTok / (kTT * 16), kSteps = kWaves / kSides;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = threadIdx.x % 16;
+    const int64_t first = (int64_t)blockIdx.x * kTok + wave % kSides * kTT * 16;
+    int rows[kTT], ids[kTT];
+    float factors[kTT];
+    bool any = false;
+#pragma unroll
+    for (int t = 0; t < kTT; ++t) {
+        rows[t] = p.row[first + t * 16 + row];
+        ids[t] = rows[t] < 0 ? -1 : p.id[first + t * 16 + row];
+        factors[t] = ids[t] < 0 ? 0.0f : p.factor[first + t * 16 + row];
+        any |= rows[t] >= 0;
+    }
+    if (!__any(any)) return;
+    const int64_t at = (int64_t)blockIdx.y * p.columns;
+    expand<T, kTT, kC, kFast>(p, rows, ids, factors, p.held + first * p.wide, at + wave / kSides * kC * 16,
+                              kSteps * kC * 16, min(at + p.columns, (int64_t)p.n));
+}
+
+template <class T, bool kBoth, int kR, int kTT, int kWaves>
+void shrink_launch(const Adapt<T>& p, uint32_t tiles, uint32_t shares, hipStream_t stream) {
+    uint32_t lds = kWaves * kR * kTT * 1024 + kTT * 16 * p.rankp * 4;
+    if (kBoth) lds += kTT * 16 * p.wide * 2;
     // more than 64 KB has to be asked for
     static const hipError_t ready = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(&adapt_tiles<T, kStage, kR, kTT, kWaves>),
+        reinterpret_cast<const void*>(&adapt_shrink<T, kBoth, kR, kTT, kWaves>),
         hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
     (void)ready;
-    adapt_tiles<T, kStage, kR, kTT, kWaves><<<dim3(tiles, shares), kWaves * 64, lds, stream>>>(p);
+    adapt_shrink<T, kBoth, kR, kTT, kWaves><<<dim3(tiles, shares), kWaves * 64, lds, stream>>>(p);
 }
 
-template <class T, int kStage, int kTT, int kWaves>
-void rank_launch(const Adapt<T>& p, uint32_t tiles, uint32_t shares, hipStream_t stream) {
-    if (kStage == kExpand || p.rankp <= 16)
-        stage_launch<T, kStage, 1, kTT, kWaves>(p, tiles, shares, stream);
+template <class T, bool kBoth, int kTT, int kWaves>
+void shrink_rank(const Adapt<T>& p, uint32_t tiles, uint32_t shares, hipStream_t stream) {
+    if (p.rankp <= 16)
+        shrink_launch<T, kBoth, 1, kTT, kWaves>(p, tiles, shares, stream);
     else if (p.rankp <= 32)
-        stage_launch<T, kStage, 2, kTT, kWaves>(p, tiles, shares, stream);
+        shrink_launch<T, kBoth, 2, kTT, kWaves>(p, tiles, shares, stream);
     else
-        stage_launch<T, kStage, 4, kTT, kWaves>(p, tiles, shares, stream);
+        shrink_launch<T, kBoth, 4, kTT, kWaves>(p, tiles, shares, stream);
 }
 
-// Rows [0, p.m) of a call, in tiles of kTT * 16; floats: the room for h.
-template <class T, int kTT, int kWaves>
-void tiles_launch(Adapt<T> p, uint64_t floats, hipStream_t stream) {
-    constexpr int kTok = kTT * 16;
-    const uint32_t grid = (uint32_t)(kTT == 1 ? p.m : groups(p.m, kTok));  // some end at once
-    const int64_t tiles = groups(p.m, kTok);
-    // columns a workgroup: enough workgroups to fill the card
-    constexpr int kCols = kWaves * (kTT == 1 ? 4 : 2) * 16;
-    const int64_t shares = std::min(groups(p.n, kCols), std::max<int64_t>(1, 1024 / tiles));
+template <class T, int kTok, int kTT, int kC>
+void expand_launch(Adapt<T> p, uint32_t grid, int64_t tiles, hipStream_t stream) {
+    constexpr int kWaves = 4, kCols = kWaves / (kTok / (kTT * 16)) * kC * 16;
+    const int64_t shares = std::min(groups(p.n, kCols), std::max<int64_t>(1, 2048 / tiles));
     p.columns = (int32_t)(groups(groups(p.n, shares), kCols) * kCols);
-    const uint32_t by = (uint32_t)groups(p.n, p.columns);
-    const int64_t units = groups(p.k, kUnit);
-    p.splits = (int32_t)std::max<int64_t>(
-        1, std::min({512 / tiles, units / (2 * kWaves), (int64_t)(floats / ((uint64_t)p.m * p.rankp))}));
-    if (floats < (uint64_t)p.m * p.rankp) {
-        p.splits = 1;
-        rank_launch<T, kBoth, kTT, kWaves>(p, grid, by, stream);
-    } else {
-        rank_launch<T, kShrink, kTT, kWaves>(p, grid, p.splits, stream);
-        rank_launch<T, kExpand, kTT, kWaves>(p, grid, by, stream);
+    const dim3 by(grid, (uint32_t)groups(p.n, p.columns));
+    const int fast = p.parts == 2 ? p.rankp : 0;
+    if (fast == 16)
+        adapt_expand<T, kTok, kTT, kC, 16, kWaves><<<by, kWaves * 64, 0, stream>>>(p);
+    else if (fast == 32)
+        adapt_expand<T, kTok, kTT, kC, 32, kWaves><<<by, kWaves * 64, 0, stream>>>(p);
+    else if (fast == 64)
+        adapt_expand<T, kTok, kTT, kC, 64, kWaves><<<by, kWaves * 64, 0, stream>>>(p);
+    else
+        adapt_expand<T, kTok, kTT, kC, 0, kWaves><<<by, kWaves * 64, 0, stream>>>(p);
+}
+
+// Floats of `work` that a tile takes beside its shares of h.
+template <class T>
+uint64_t tile_floats(const Adapt<T>& p, int rows) {
+    return rows * (p.wide / 2 + 3);
+}
+
+// Rows [0, p.m) of a call; floats: the room in `work`.
+template <class T, int kTT, int kWaves>
+void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
+    constexpr int kTok = kTT * 16;
+    int64_t tiles = groups(p.m, kTok);  // at least
+    int64_t grid = tiles;
+    if (kTT == 1) {
+        grid = p.count < kCounted ? std::min<int64_t>(p.m, p.m / kTok + p.count + 1) : p.m;
+        tiles = std::min<int64_t>(grid, tiles + p.count);
     }
+    const uint64_t sums = (uint64_t)kTok * p.rankp, each = tile_floats(p, kTok);
+    if (floats < grid * each) {
+        constexpr int kCols = kWaves * (kTT == 1 ? 4 : 2) * 16;
+        const int64_t shares = std::min(groups(p.n, kCols), std::max<int64_t>(1, 1024 / tiles));
+        p.columns = (int32_t)(groups(groups(p.n, shares), kCols) * kCols);
+        p.splits = 1;
+        return shrink_rank<T, true, kTT, kWaves>(p, (uint32_t)grid, (uint32_t)groups(p.n, p.columns), stream);
+    }
+    // workgroups that share a tile's k: to fill the card, each wave left with
+    // two rounds of loads or more
+    const int64_t room = (floats - grid * each) / (grid * sums);
+    p.splits = (int32_t)std::max<int64_t>(1, std::min({512 / tiles, groups(p.k, kUnit) / (2 * kWaves), room}));
+    if (grid > (int64_t)kWorkCounters) p.splits = 1;
+    p.counters = reinterpret_cast<uint32_t*>(work);
+    p.held = reinterpret_cast<T*>(work + kWorkHead);
+    p.factor = reinterpret_cast<float*>(p.held + grid * kTok * p.wide);
+    p.row = reinterpret_cast<int32_t*>(p.factor + grid * kTok);
+    p.id = p.row + grid * kTok;
+    p.partial = reinterpret_cast<float*>(p.id + grid * kTok);
+    shrink_rank<T, false, kTT, kWaves>(p, (uint32_t)grid, p.splits, stream);
+    expand_launch<T, kTok, kTT == 1 ? 1 : 2, 4>(p, (uint32_t)grid, tiles, stream);
 }
 
 template <class T>
@@ -469,14 +658,12 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
     p.b_words = words(a.b, p.b_stride) && words(a.b, p.b_row);
     p.quads = quad(a.out, p.out_stride, p.out_f32 ? 4 : 2) && quad(a.base, p.base_stride, p.base_f32 ? 4 : 2);
     uint64_t floats = 0;
-    if (a.work_bytes > kWorkHead) {
-        p.h = reinterpret_cast<float*>(static_cast<char*>(a.work) + kWorkHead);
+    if (a.work_bytes > kWorkHead)
         floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
-    }
-    // rows that are gathered, or whose h there is room for, at once
+    // rows that are gathered, or whose tiles there is room for, at once
     int64_t rows = many ? a.m : std::min<int64_t>(a.m, kGathered);
-    if (many && floats >= (uint64_t)64 * p.rankp)
-        rows = std::min<int64_t>(rows, floats / p.rankp / 64 * 64);
+    if (many && floats >= tile_floats(p, 64))
+        rows = std::min<int64_t>(rows, floats / tile_floats(p, 64) * 64);
     for (int64_t i = 0; i < a.m; i += rows) {
         p.m = (int32_t)std::min(rows, a.m - i);
         p.x = static_cast<const T*>(a.x) + i * p.x_stride;
@@ -487,9 +674,9 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
         p.base = at(a.base, p.base_stride, p.base_f32);
         p.out = const_cast<char*>(at(a.out, p.out_stride, p.out_f32));
         if (many)
-            tiles_launch<T, 4, 4>(p, floats, stream);
+            tiles_launch<T, 4, 4>(p, static_cast<char*>(a.work), floats, stream);
         else
-            tiles_launch<T, 1, 8>(p, floats, stream);
+            tiles_launch<T, 1, 8>(p, static_cast<char*>(a.work), floats, stream);
     }
     return launched("ii_adapt");
 }
