@@ -4,7 +4,7 @@
 // Rows of one adapter share what is read of it, so rows are taken in tiles of
 // one adapter. A few rows, in any order, are gathered: a workgroup counts the
 // rows of each adapter and finds which of them its tile of 16 has. Of many rows,
-// which come in runs, a tile is 64 neighbours, with a pass for each adapter among
+// which come in runs, a tile is 32 neighbours, with a pass for each adapter among
 // them.
 //
 // h = A x is a sum over k that the waves of a workgroup, and workgroups, share.
@@ -294,38 +294,41 @@ __device__ inline void cut(const Adapt<T>& p, Tile<kTok>& tile, const float* h, 
     __syncthreads();
 }
 
-// Columns j .. j + 3 of a row of base as they lie there; of out.
-template <class T>
-__device__ inline u32x4 base_of(const Adapt<T>& p, int64_t row, int64_t j) {
+enum { kNoBase, kBaseT, kBaseF32 };
+
+// Columns j .. j + 3 of a row of base as they lie there, of out; `whole`: they are
+// all there, and words.
+template <class T, int kBase>
+__device__ inline u32x4 base_of(const Adapt<T>& p, int64_t row, int64_t j, bool whole) {
     u32x4 v = {};
     const int64_t at = row * p.base_stride + j;
-    if (p.quads && j + 4 <= p.n) {
-        if (p.base_f32) return *reinterpret_cast<const u32x4*>(static_cast<const float*>(p.base) + at);
+    if (kBase == kNoBase) return v;
+    if (whole) {
+        if (kBase == kBaseF32) return *reinterpret_cast<const u32x4*>(static_cast<const float*>(p.base) + at);
         const u32x2 half = *reinterpret_cast<const u32x2*>(static_cast<const T*>(p.base) + at);
         return u32x4{half[0], half[1], 0, 0};
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         if (j + r >= p.n) break;
-        if (p.base_f32)
+        if (kBase == kBaseF32)
             v[r] = static_cast<const uint32_t*>(p.base)[at + r];
         else
             v[r / 2] |= (uint32_t)static_cast<const uint16_t*>(p.base)[at + r] << r % 2 * 16;
     }
     return v;
 }
-template <class T>
-__device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 y, u32x4 base) {
+template <class T, int kBase>
+__device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 y, u32x4 base, bool whole) {
     using x4 = typename Vec<T>::x4;
-    if (p.base && p.base_f32) {
+    if (kBase == kBaseF32) {
         y += __builtin_bit_cast(f32x4, base);
-    } else if (p.base) {
+    } else if (kBase == kBaseT) {
         const x4 v = __builtin_bit_cast(x4, u32x2{base[0], base[1]});
 #pragma unroll
         for (int r = 0; r < 4; ++r) y[r] += (float)v[r];
     }
     const int64_t at = row * p.out_stride + j;
-    const bool whole = p.quads && j + 4 <= p.n;
     if (p.out_f32) {
         float* out = static_cast<float*>(p.out) + at;
         if (whole) {
@@ -354,18 +357,19 @@ __device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 y, u
 // rows of out that a wave has: of each 16, lane l has row l mod 16, of which
 // `rows`, `ids` and `factors` are told, and `parts` is h cut, [row][wide]. kFast:
 // rankp, if a row's parts are two and stay in registers (0: neither).
-template <class T, int kTT, int kC, int kFast>
+template <class T, int kTT, int kC, int kFast, int kBase>
 __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const int (&ids)[kTT],
                               const float (&factors)[kTT], const T* parts, int64_t first, int64_t step,
                               int64_t end) {
     using x8 = typename Vec<T>::x8;
     const int lane = threadIdx.x % 64, row = lane % 16, part = lane / 16;
     const int held = p.parts * p.rankp;
-    constexpr int kSteps = kFast ? kFast * 2 / 32 : 1;
-    x8 hv[kSteps][kTT];
+    // what a part's steps read of B; both parts of 16 go into one instruction
+    constexpr int kSteps = kFast > 16 ? kFast / 32 : 1, kTimes = kFast > 16 ? 2 : 1;
+    x8 hv[kTimes * kSteps][kTT];
     if constexpr (kFast != 0)
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+        for (int s = 0; s < kTimes * kSteps; ++s)
 #pragma unroll
             for (int t = 0; t < kTT; ++t)
                 hv[s][t] = *reinterpret_cast<const x8*>(parts + (t * 16 + row) * p.wide + s * 32 + part * 8);
@@ -378,60 +382,97 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
         for (int d = 1; d < 16; d *= 2) v = min(v, __shfl_xor(v, d));
         return __builtin_amdgcn_readfirstlane(v);
     };
-    for (int64_t n0 = first; n0 < end; n0 += step) {
-        u32x4 base[kC][kTT];
-        if (p.base)
+    // base is asked for a step ahead, behind what is read of B; alike in all
+    // lanes, so that no branch comes between the loads
+    u32x4 base[kC][kTT], ahead[kC][kTT];
+    const auto whole = [&](int64_t n0) { return p.quads && n0 + kC * 16 <= p.n; };
+    const auto ask = [&](int64_t n0) {
+        if (kBase == kNoBase || n0 >= end) return;
+        if (whole(n0)) {
 #pragma unroll
             for (int t = 0; t < kTT; ++t)
 #pragma unroll
-                for (int c = 0; c < kC; ++c) {
-                    base[c][t] = u32x4{};
-                    if (rows[t] >= 0) base[c][t] = base_of(p, rows[t], n0 + c * 16 + part * 4);
-                }
+                for (int c = 0; c < kC; ++c)
+                    ahead[c][t] = base_of<T, kBase>(p, max(rows[t], 0), n0 + c * 16 + part * 4, true);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kTT; ++t)
+#pragma unroll
+                for (int c = 0; c < kC; ++c)
+                    ahead[c][t] = base_of<T, kBase>(p, max(rows[t], 0), n0 + c * 16 + part * 4, false);
+        }
+    };
+    const int a0 = next(-1);
+    ask(first);
+    for (int64_t n0 = first; n0 < end; n0 += step) {
+#pragma unroll
+        for (int t = 0; t < kTT; ++t)
+#pragma unroll
+            for (int c = 0; c < kC; ++c) base[c][t] = ahead[c][t];
+        bool asked = false;
         f32x4 total[kC][kTT] = {};
-        for (int a = next(-1); a != INT32_MAX; a = next(a)) {
+        for (int a = a0; a != INT32_MAX; a = next(a)) {
             const int rank = rank_of(p, a);
             const T* b[kC];
 #pragma unroll
             for (int c = 0; c < kC; ++c)
                 b[c] = p.b + a * p.b_stride + min(n0 + c * 16 + row, (int64_t)p.n - 1) * p.b_row;
             f32x4 acc[kC][kTT] = {};
-            if constexpr (kFast == 16) {
-                // both parts in one instruction
-                const int col = part % 2 * 8;
+            const bool words = p.b_words && rank % 8 == 0 && rank > 0;
+            if constexpr (kFast != 0) {
+                x8 bv[kC][kSteps];
+                if (words) {
 #pragma unroll
-                for (int c = 0; c < kC; ++c) {
-                    const x8 bv = some(b[c] + col, rank - col, p.b_words);
+                    for (int c = 0; c < kC; ++c)
 #pragma unroll
-                    for (int t = 0; t < kTT; ++t) acc[c][t] = mfma16(bv, hv[0][t], acc[c][t]);
+                        for (int s = 0; s < kSteps; ++s) {
+                            const int col = (s * 32 + part * 8) % kFast;
+                            bv[c][s] = *reinterpret_cast<const x8*>(b[c] + (col < rank ? col : 0));
+                        }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < kC; ++c)
+#pragma unroll
+                        for (int s = 0; s < kSteps; ++s) {
+                            const int col = (s * 32 + part * 8) % kFast;
+                            bv[c][s] = some(b[c] + col, rank - col, false);
+                        }
                 }
-            } else if constexpr (kFast != 0) {
-                x8 bv[kC][kSteps / 2];
+                if (!asked) ask(n0 + step);
+                asked = true;
+                if (rank < kFast)
 #pragma unroll
-                for (int c = 0; c < kC; ++c)
+                    for (int c = 0; c < kC; ++c)
 #pragma unroll
-                    for (int s = 0; s < kSteps / 2; ++s) {
-                        const int col = s * 32 + part * 8;
-                        bv[c][s] = some(b[c] + col, rank - col, p.b_words);
-                    }
+                        for (int s = 0; s < kSteps; ++s)
+                            if ((s * 32 + part * 8) % kFast >= rank) bv[c][s] = x8{};
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s)
+                for (int s = 0; s < kTimes * kSteps; ++s)
 #pragma unroll
                     for (int c = 0; c < kC; ++c)
 #pragma unroll
                         for (int t = 0; t < kTT; ++t)
-                            acc[c][t] = mfma16(bv[c][s % (kSteps / 2)], hv[s][t], acc[c][t]);
+                            acc[c][t] = mfma16(bv[c][s % kSteps], hv[s][t], acc[c][t]);
             } else {
                 int col = part * 8;
                 while (col >= p.rankp) col -= p.rankp;
                 for (int at = part * 8; at < p.wide; at += 32) {
+                    const bool there = at < held && col < rank;
                     x8 bv[kC], h[kTT];
+                    if (words) {
 #pragma unroll
-                    for (int c = 0; c < kC; ++c)
-                        bv[c] = some(b[c] + col, at < held ? rank - col : 0, p.b_words);
+                        for (int c = 0; c < kC; ++c)
+                            bv[c] = *reinterpret_cast<const x8*>(b[c] + (there ? col : 0));
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < kC; ++c) bv[c] = some(b[c] + col, rank - col, false);
+                    }
 #pragma unroll
                     for (int t = 0; t < kTT; ++t)
                         h[t] = *reinterpret_cast<const x8*>(parts + (t * 16 + row) * p.wide + at);
+#pragma unroll
+                    for (int c = 0; c < kC; ++c)
+                        if (!there) bv[c] = x8{};
 #pragma unroll
                     for (int c = 0; c < kC; ++c)
 #pragma unroll
@@ -439,20 +480,32 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
                     col += 32;
                     while (col >= p.rankp) col -= p.rankp;
                 }
+                if (!asked) ask(n0 + step);
+                asked = true;
             }
             // a row has one adapter; what others have there does not matter
 #pragma unroll
             for (int t = 0; t < kTT; ++t)
-                if (ids[t] == a)
-#pragma unroll
-                    for (int c = 0; c < kC; ++c) total[c][t] = acc[c][t] * factors[t];
-        }
-#pragma unroll
-        for (int t = 0; t < kTT; ++t)
-            if (rows[t] >= 0)
 #pragma unroll
                 for (int c = 0; c < kC; ++c)
-                    put(p, rows[t], n0 + c * 16 + part * 4, total[c][t], base[c][t]);
+                    total[c][t] = ids[t] == a ? acc[c][t] * factors[t] : total[c][t];
+        }
+        if (!asked) ask(n0 + step);
+        if (whole(n0)) {
+#pragma unroll
+            for (int t = 0; t < kTT; ++t)
+                if (rows[t] >= 0)
+#pragma unroll
+                    for (int c = 0; c < kC; ++c)
+                        put<T, kBase>(p, rows[t], n0 + c * 16 + part * 4, total[c][t], base[c][t], true);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kTT; ++t)
+                if (rows[t] >= 0)
+#pragma unroll
+                    for (int c = 0; c < kC; ++c)
+                        put<T, kBase>(p, rows[t], n0 + c * 16 + part * 4, total[c][t], base[c][t], false);
+        }
     }
 }
 
@@ -496,8 +549,14 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
         }
         constexpr int kC = kTT == 1 ? 4 : 2;
         const int64_t at = (int64_t)blockIdx.y * p.columns;
-        expand<T, kTT, kC, 0>(p, rows, ids, factors, parts, at + threadIdx.x / 64 * kC * 16,
-                              kWaves * kC * 16, min(at + p.columns, (int64_t)p.n));
+        const int64_t from = at + threadIdx.x / 64 * kC * 16, end = min(at + p.columns, (int64_t)p.n);
+        constexpr int kStep = kWaves * kC * 16;
+        if (!p.base)
+            expand<T, kTT, kC, 0, kNoBase>(p, rows, ids, factors, parts, from, kStep, end);
+        else if (p.base_f32)
+            expand<T, kTT, kC, 0, kBaseF32>(p, rows, ids, factors, parts, from, kStep, end);
+        else
+            expand<T, kTT, kC, 0, kBaseT>(p, rows, ids, factors, parts, from, kStep, end);
     } else {
         if (p.splits > 1) {
             const Rsrc parts = buffer(p.partial + (int64_t)blockIdx.x * p.splits * sums,
@@ -522,13 +581,13 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
     }
 }
 
-// Columns of tile blockIdx.x from what adapt_shrink left: of a workgroup's waves
+// Columns of tile blockIdx.y from what adapt_shrink left: of a workgroup's waves
 // kTok / (kTT * 16) share its rows, the others its columns.
-template <class T, int kTok, int kTT, int kC, int kFast, int kWaves>
+template <class T, int kTok, int kTT, int kC, int kFast, int kBase, int kWaves>
 __global__ __launch_bounds__(kWaves * 64) void adapt_expand(Adapt<T> p) {
     constexpr int kSides = kTok / (kTT * 16), kSteps = kWaves / kSides;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = threadIdx.x % 16;
-    const int64_t first = (int64_t)blockIdx.x * kTok + wave % kSides * kTT * 16;
+    const int64_t first = (int64_t)blockIdx.y * kTok + wave % kSides * kTT * 16;
     int rows[kTT], ids[kTT];
     float factors[kTT];
     bool any = false;
@@ -540,9 +599,10 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_expand(Adapt<T> p) {
         any |= rows[t] >= 0;
     }
     if (!__any(any)) return;
-    const int64_t at = (int64_t)blockIdx.y * p.columns;
-    expand<T, kTT, kC, kFast>(p, rows, ids, factors, p.held + first * p.wide, at + wave / kSides * kC * 16,
-                              kSteps * kC * 16, min(at + p.columns, (int64_t)p.n));
+    const int64_t at = (int64_t)blockIdx.x * p.columns;
+    expand<T, kTT, kC, kFast, kBase>(p, rows, ids, factors, p.held + first * p.wide,
+                                     at + wave / kSides * kC * 16, kSteps * kC * 16,
+                                     min(at + p.columns, (int64_t)p.n));
 }
 
 template <class T, bool kBoth, int kR, int kTT, int kWaves>
@@ -567,21 +627,30 @@ void shrink_rank(const Adapt<T>& p, uint32_t tiles, uint32_t shares, hipStream_t
         shrink_launch<T, kBoth, 4, kTT, kWaves>(p, tiles, shares, stream);
 }
 
+template <class T, int kTok, int kTT, int kC, int kFast>
+void expand_base(const Adapt<T>& p, dim3 grid, hipStream_t stream) {
+    constexpr int kWaves = 4;
+    if (!p.base)
+        adapt_expand<T, kTok, kTT, kC, kFast, kNoBase, kWaves><<<grid, kWaves * 64, 0, stream>>>(p);
+    else if (p.base_f32)
+        adapt_expand<T, kTok, kTT, kC, kFast, kBaseF32, kWaves><<<grid, kWaves * 64, 0, stream>>>(p);
+    else
+        adapt_expand<T, kTok, kTT, kC, kFast, kBaseT, kWaves><<<grid, kWaves * 64, 0, stream>>>(p);
+}
+
 template <class T, int kTok, int kTT, int kC>
 void expand_launch(Adapt<T> p, uint32_t grid, int64_t tiles, hipStream_t stream) {
     constexpr int kWaves = 4, kCols = kWaves / (kTok / (kTT * 16)) * kC * 16;
     const int64_t shares = std::min(groups(p.n, kCols), std::max<int64_t>(1, 2048 / tiles));
     p.columns = (int32_t)(groups(groups(p.n, shares), kCols) * kCols);
-    const dim3 by(grid, (uint32_t)groups(p.n, p.columns));
+    // the columns of a tile one after another: rows whose length is a multiple of
+    // many channels' width are read along, not across
+    const dim3 by((uint32_t)groups(p.n, p.columns), grid);
     const int fast = p.parts == 2 ? p.rankp : 0;
-    if (fast == 16)
-        adapt_expand<T, kTok, kTT, kC, 16, kWaves><<<by, kWaves * 64, 0, stream>>>(p);
-    else if (fast == 32)
-        adapt_expand<T, kTok, kTT, kC, 32, kWaves><<<by, kWaves * 64, 0, stream>>>(p);
-    else if (fast == 64)
-        adapt_expand<T, kTok, kTT, kC, 64, kWaves><<<by, kWaves * 64, 0, stream>>>(p);
-    else
-        adapt_expand<T, kTok, kTT, kC, 0, kWaves><<<by, kWaves * 64, 0, stream>>>(p);
+    if (fast == 16) return expand_base<T, kTok, kTT, kC, 16>(p, by, stream);
+    if (fast == 32) return expand_base<T, kTok, kTT, kC, 32>(p, by, stream);
+    if (fast == 64) return expand_base<T, kTok, kTT, kC, 64>(p, by, stream);
+    expand_base<T, kTok, kTT, kC, 0>(p, by, stream);
 }
 
 // Floats of `work` that a tile takes beside its shares of h.
@@ -662,8 +731,8 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
         floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
     // rows that are gathered, or whose tiles there is room for, at once
     int64_t rows = many ? a.m : std::min<int64_t>(a.m, kGathered);
-    if (many && floats >= tile_floats(p, 64))
-        rows = std::min<int64_t>(rows, floats / tile_floats(p, 64) * 64);
+    if (many && floats >= tile_floats(p, 32))
+        rows = std::min<int64_t>(rows, floats / tile_floats(p, 32) * 32);
     for (int64_t i = 0; i < a.m; i += rows) {
         p.m = (int32_t)std::min(rows, a.m - i);
         p.x = static_cast<const T*>(a.x) + i * p.x_stride;
@@ -674,7 +743,7 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
         p.base = at(a.base, p.base_stride, p.base_f32);
         p.out = const_cast<char*>(at(a.out, p.out_stride, p.out_f32));
         if (many)
-            tiles_launch<T, 4, 4>(p, static_cast<char*>(a.work), floats, stream);
+            tiles_launch<T, 2, 4>(p, static_cast<char*>(a.work), floats, stream);
         else
             tiles_launch<T, 1, 8>(p, static_cast<char*>(a.work), floats, stream);
     }
