@@ -44,8 +44,9 @@ struct Adapt {
     int32_t rankp;        // rank in whole words of 8
     int32_t parts, wide;  // parts of h; elements of a row of parts in LDS
     int32_t columns;      // of out, a workgroup's
-    int32_t splits;       // workgroups that share k
-    bool out_f32, base_f32, words, b_words, quads;
+    int32_t tiles, splits;  // workgroups that share k of a tile
+    int32_t shares;       // workgroups that share its columns
+    bool out_f32, base_f32, words, b_words, words_out;
     uint32_t* counters;
     float* partial;       // [tiles][splits][rows of a tile][rankp]
     // what the first kernel leaves of each row of each tile
@@ -71,6 +72,20 @@ struct Tile {
     int row[kTok], id[kTok];
     float factor[kTok];  // of a result
 };
+
+// A workgroup's tile, and which of those that share it this is. The workgroups of
+// a tile's columns are neighbours, so that its rows are read and written along;
+// those of a tile's k are not. All on one XCD, so that its L2 need not hold every
+// adapter, took 4099 rows x 4096 x 14336 from 122 us to 132.
+struct Share {
+    int tile, share;
+};
+__device__ inline Share share_of_columns(int shares) {
+    return {(int)(blockIdx.x / shares), (int)(blockIdx.x % shares)};
+}
+__device__ inline Share share_of_k(int tiles) {
+    return {(int)(blockIdx.x % tiles), (int)(blockIdx.x / tiles)};
+}
 
 // The rows of tile t of the gathered ones, false if there is none. Called by all
 // threads.
@@ -183,7 +198,8 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
                               float* red, Keep&& keep) {
     using x8 = typename Vec<T>::x8;
     constexpr int kSums = kR * kTT * 256;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, part = lane / 16;
+    const int lane = threadIdx.x % 64, row = lane % 16, part = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int rank = rank_of(p, a);
     const T *ap[kR], *xp[kTT];
 #pragma unroll
@@ -195,7 +211,7 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
     const int units = (int)groups(p.k, kUnit), whole = p.words ? p.k / kUnit : 0;
     const int step = kWaves * p.splits;
     int u = split * kWaves + wave;
-    constexpr int kAhead = kTT > 1 ? 2 : 4;
+    constexpr int kAhead = kTT > 1 ? 2 : 4;  // units whose loads are on their way
     const auto take = [&](int u, x8(&av)[2][kR], x8(&xv)[2][kTT]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -296,59 +312,68 @@ __device__ inline void cut(const Adapt<T>& p, Tile<kTok>& tile, const float* h, 
 
 enum { kNoBase, kBaseT, kBaseF32 };
 
-// Columns j .. j + 3 of a row of base as they lie there, of out; `whole`: they are
-// all there, and words.
+// Eight columns of a row of base as they lie there.
 template <class T, int kBase>
-__device__ inline u32x4 base_of(const Adapt<T>& p, int64_t row, int64_t j, bool whole) {
-    u32x4 v = {};
+struct Base {
+    u32x4 word[kBase == kBaseF32 ? 2 : 1];
+};
+// Columns j .. j + 7 of a row of base, and of out; `whole`: they are all there, and
+// words.
+template <class T, int kBase>
+__device__ inline void base_of(const Adapt<T>& p, int64_t row, int64_t j, bool whole, Base<T, kBase>& v) {
     const int64_t at = row * p.base_stride + j;
-    if (kBase == kNoBase) return v;
-    if (whole) {
-        if (kBase == kBaseF32) return *reinterpret_cast<const u32x4*>(static_cast<const float*>(p.base) + at);
-        const u32x2 half = *reinterpret_cast<const u32x2*>(static_cast<const T*>(p.base) + at);
-        return u32x4{half[0], half[1], 0, 0};
-    }
+    if constexpr (kBase == kBaseF32) {
+        const float* from = static_cast<const float*>(p.base) + at;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (j + r >= p.n) break;
-        if (kBase == kBaseF32)
-            v[r] = static_cast<const uint32_t*>(p.base)[at + r];
-        else
-            v[r / 2] |= (uint32_t)static_cast<const uint16_t*>(p.base)[at + r] << r % 2 * 16;
+        for (int h = 0; h < 2; ++h) {
+            if (whole) {
+                v.word[h] = reinterpret_cast<const u32x4*>(from)[h];
+            } else {
+                v.word[h] = u32x4{};
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (j + h * 4 + r < p.n) v.word[h][r] = __builtin_bit_cast(uint32_t, from[h * 4 + r]);
+            }
+        }
+    } else if constexpr (kBase == kBaseT) {
+        v.word[0] = __builtin_bit_cast(u32x4, some(static_cast<const T*>(p.base) + at, p.n - j, whole));
     }
-    return v;
 }
 template <class T, int kBase>
-__device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 y, u32x4 base, bool whole) {
-    using x4 = typename Vec<T>::x4;
-    if (kBase == kBaseF32) {
-        y += __builtin_bit_cast(f32x4, base);
-    } else if (kBase == kBaseT) {
-        const x4 v = __builtin_bit_cast(x4, u32x2{base[0], base[1]});
+__device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 low, f32x4 high,
+                           const Base<T, kBase>& base, bool whole) {
+    using x8 = typename Vec<T>::x8;
+    float y[8];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] += (float)v[r];
+    for (int r = 0; r < 8; ++r) {
+        y[r] = r < 4 ? low[r] : high[r - 4];
+        if constexpr (kBase == kBaseF32)
+            y[r] += __builtin_bit_cast(float, (uint32_t)base.word[r / 4][r % 4]);
+        else if constexpr (kBase == kBaseT)
+            y[r] += (float)__builtin_bit_cast(x8, base.word[0])[r];
     }
     const int64_t at = row * p.out_stride + j;
     if (p.out_f32) {
         float* out = static_cast<float*>(p.out) + at;
         if (whole) {
-            *reinterpret_cast<f32x4*>(out) = y;
+            reinterpret_cast<f32x4*>(out)[0] = f32x4{y[0], y[1], y[2], y[3]};
+            reinterpret_cast<f32x4*>(out)[1] = f32x4{y[4], y[5], y[6], y[7]};
             return;
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 8; ++r)
             if (j + r < p.n) out[r] = y[r];
     } else {
         T* out = static_cast<T*>(p.out) + at;
-        x4 v;
+        x8 v;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = (T)y[r];
+        for (int r = 0; r < 8; ++r) v[r] = (T)y[r];
         if (whole) {
-            *reinterpret_cast<x4*>(out) = v;
+            *reinterpret_cast<x8*>(out) = v;
             return;
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 8; ++r)
             if (j + r < p.n) out[r] = v[r];
     }
 }
@@ -357,13 +382,16 @@ __device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 y, u
 // rows of out that a wave has: of each 16, lane l has row l mod 16, of which
 // `rows`, `ids` and `factors` are told, and `parts` is h cut, [row][wide]. kFast:
 // rankp, if a row's parts are two and stay in registers (0: neither).
+//
+// Of two products of 16 columns a lane gets four columns each; the rows of B are
+// given to them so that these are eight neighbours, a word of out.
 template <class T, int kTT, int kC, int kFast, int kBase>
 __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const int (&ids)[kTT],
                               const float (&factors)[kTT], const T* parts, int64_t first, int64_t step,
                               int64_t end) {
     using x8 = typename Vec<T>::x8;
     const int lane = threadIdx.x % 64, row = lane % 16, part = lane / 16;
-    const int held = p.parts * p.rankp;
+    const int held = p.parts * p.rankp, place = row / 4 * 8 + row % 4;
     // what a part's steps read of B; both parts of 16 go into one instruction
     constexpr int kSteps = kFast > 16 ? kFast / 32 : 1, kTimes = kFast > 16 ? 2 : 1;
     x8 hv[kTimes * kSteps][kTT];
@@ -384,22 +412,23 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
     };
     // base is asked for a step ahead, behind what is read of B; alike in all
     // lanes, so that no branch comes between the loads
-    u32x4 base[kC][kTT], ahead[kC][kTT];
-    const auto whole = [&](int64_t n0) { return p.quads && n0 + kC * 16 <= p.n; };
+    static_assert(kC % 2 == 0);
+    Base<T, kBase> base[kC / 2][kTT], ahead[kC / 2][kTT];
+    const auto whole = [&](int64_t n0) { return p.words_out && n0 + kC * 16 <= p.n; };
     const auto ask = [&](int64_t n0) {
         if (kBase == kNoBase || n0 >= end) return;
         if (whole(n0)) {
 #pragma unroll
             for (int t = 0; t < kTT; ++t)
 #pragma unroll
-                for (int c = 0; c < kC; ++c)
-                    ahead[c][t] = base_of<T, kBase>(p, max(rows[t], 0), n0 + c * 16 + part * 4, true);
+                for (int c = 0; c < kC / 2; ++c)
+                    base_of(p, max(rows[t], 0), n0 + c * 32 + part * 8, true, ahead[c][t]);
         } else {
 #pragma unroll
             for (int t = 0; t < kTT; ++t)
 #pragma unroll
-                for (int c = 0; c < kC; ++c)
-                    ahead[c][t] = base_of<T, kBase>(p, max(rows[t], 0), n0 + c * 16 + part * 4, false);
+                for (int c = 0; c < kC / 2; ++c)
+                    base_of(p, max(rows[t], 0), n0 + c * 32 + part * 8, false, ahead[c][t]);
         }
     };
     const int a0 = next(-1);
@@ -408,7 +437,7 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
 #pragma unroll
         for (int t = 0; t < kTT; ++t)
 #pragma unroll
-            for (int c = 0; c < kC; ++c) base[c][t] = ahead[c][t];
+            for (int c = 0; c < kC / 2; ++c) base[c][t] = ahead[c][t];
         bool asked = false;
         f32x4 total[kC][kTT] = {};
         for (int a = a0; a != INT32_MAX; a = next(a)) {
@@ -416,7 +445,7 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
             const T* b[kC];
 #pragma unroll
             for (int c = 0; c < kC; ++c)
-                b[c] = p.b + a * p.b_stride + min(n0 + c * 16 + row, (int64_t)p.n - 1) * p.b_row;
+                b[c] = p.b + a * p.b_stride + min(n0 + c / 2 * 32 + place + c % 2 * 4, (int64_t)p.n - 1) * p.b_row;
             f32x4 acc[kC][kTT] = {};
             const bool words = p.b_words && rank % 8 == 0 && rank > 0;
             if constexpr (kFast != 0) {
@@ -496,20 +525,22 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
             for (int t = 0; t < kTT; ++t)
                 if (rows[t] >= 0)
 #pragma unroll
-                    for (int c = 0; c < kC; ++c)
-                        put<T, kBase>(p, rows[t], n0 + c * 16 + part * 4, total[c][t], base[c][t], true);
+                    for (int c = 0; c < kC / 2; ++c)
+                        put(p, rows[t], n0 + c * 32 + part * 8, total[c * 2][t], total[c * 2 + 1][t],
+                            base[c][t], true);
         } else {
 #pragma unroll
             for (int t = 0; t < kTT; ++t)
                 if (rows[t] >= 0)
 #pragma unroll
-                    for (int c = 0; c < kC; ++c)
-                        put<T, kBase>(p, rows[t], n0 + c * 16 + part * 4, total[c][t], base[c][t], false);
+                    for (int c = 0; c < kC / 2; ++c)
+                        put(p, rows[t], n0 + c * 32 + part * 8, total[c * 2][t], total[c * 2 + 1][t],
+                            base[c][t], false);
         }
     }
 }
 
-// h of tile blockIdx.x, cut: in LDS, formed by each of the workgroups that share
+// h of a tile, cut: in LDS, formed by each of the workgroups that share
 // the tile's columns, which follow (kBoth); or in memory, by the last to arrive of
 // those that share k.
 template <class T, bool kBoth, int kR, int kTT, int kWaves>
@@ -517,14 +548,15 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
     constexpr int kTok = kTT * 16, kThreads = kWaves * 64;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Tile<kTok> tile;
-    const int64_t first = (int64_t)blockIdx.x * kTok;  // of the rows in memory
+    const Share mine = kBoth ? share_of_columns(p.shares) : share_of_k(p.tiles);
+    const int64_t first = (int64_t)mine.tile * kTok;  // of the rows in memory
     if constexpr (kTT == 1) {
-        if (!gather(p, blockIdx.x, tile)) {
-            if (!kBoth && blockIdx.y == 0 && threadIdx.x < kTok) p.row[first + threadIdx.x] = -1;
+        if (!gather(p, mine.tile, tile)) {
+            if (!kBoth && mine.share == 0 && threadIdx.x < kTok) p.row[first + threadIdx.x] = -1;
             return;
         }
     } else {
-        neighbours(p, blockIdx.x, tile);
+        neighbours(p, mine.tile, tile);
     }
     float* red = reinterpret_cast<float*>(lds);
     float* h = red + kWaves * kR * kTT * 256;
@@ -533,7 +565,7 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
     __syncthreads();
     for (int a = next_adapter(tile, -1); a != INT32_MAX; a = next_adapter(tile, a))
         for (int r0 = 0; r0 < p.rankp; r0 += kR * 16)
-            shrink<T, kR, kTT, kWaves>(p, tile, a, r0, kBoth ? 0 : blockIdx.y, red,
+            shrink<T, kR, kTT, kWaves>(p, tile, a, r0, kBoth ? 0 : mine.share, red,
                                        [&](int token, int r, float v) { h[token * p.rankp + r] = v; });
     if constexpr (kBoth) {
         T* parts = reinterpret_cast<T*>(h + sums);
@@ -548,7 +580,7 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
             factors[t] = tile.factor[t * 16 + row];
         }
         constexpr int kC = kTT == 1 ? 4 : 2;
-        const int64_t at = (int64_t)blockIdx.y * p.columns;
+        const int64_t at = (int64_t)mine.share * p.columns;
         const int64_t from = at + threadIdx.x / 64 * kC * 16, end = min(at + p.columns, (int64_t)p.n);
         constexpr int kStep = kWaves * kC * 16;
         if (!p.base)
@@ -559,11 +591,11 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
             expand<T, kTT, kC, 0, kBaseT>(p, rows, ids, factors, parts, from, kStep, end);
     } else {
         if (p.splits > 1) {
-            const Rsrc parts = buffer(p.partial + (int64_t)blockIdx.x * p.splits * sums,
+            const Rsrc parts = buffer(p.partial + (int64_t)mine.tile * p.splits * sums,
                                       (int64_t)p.splits * sums * 4);
             for (int e = threadIdx.x * 4; e < sums; e += kThreads * 4)
-                leave_part(parts, (blockIdx.y * sums + e) * 4, *reinterpret_cast<f32x4*>(h + e));
-            if (!arrive_last(&p.counters[blockIdx.x], p.splits)) return;
+                leave_part(parts, (mine.share * sums + e) * 4, *reinterpret_cast<f32x4*>(h + e));
+            if (!arrive_last(&p.counters[mine.tile], p.splits)) return;
             for (int e = threadIdx.x * 4; e < sums; e += kThreads * 4) {
                 f32x4 s = {};
 #pragma unroll 8
@@ -581,13 +613,14 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
     }
 }
 
-// Columns of tile blockIdx.y from what adapt_shrink left: of a workgroup's waves
+// Columns of a tile from what adapt_shrink left: of a workgroup's waves
 // kTok / (kTT * 16) share its rows, the others its columns.
 template <class T, int kTok, int kTT, int kC, int kFast, int kBase, int kWaves>
 __global__ __launch_bounds__(kWaves * 64) void adapt_expand(Adapt<T> p) {
     constexpr int kSides = kTok / (kTT * 16), kSteps = kWaves / kSides;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = threadIdx.x % 16;
-    const int64_t first = (int64_t)blockIdx.y * kTok + wave % kSides * kTT * 16;
+    const Share mine = share_of_columns(p.shares);
+    const int64_t first = (int64_t)mine.tile * kTok + wave % kSides * kTT * 16;
     int rows[kTT], ids[kTT];
     float factors[kTT];
     bool any = false;
@@ -599,14 +632,14 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_expand(Adapt<T> p) {
         any |= rows[t] >= 0;
     }
     if (!__any(any)) return;
-    const int64_t at = (int64_t)blockIdx.x * p.columns;
+    const int64_t at = (int64_t)mine.share * p.columns;
     expand<T, kTT, kC, kFast, kBase>(p, rows, ids, factors, p.held + first * p.wide,
                                      at + wave / kSides * kC * 16, kSteps * kC * 16,
                                      min(at + p.columns, (int64_t)p.n));
 }
 
 template <class T, bool kBoth, int kR, int kTT, int kWaves>
-void shrink_launch(const Adapt<T>& p, uint32_t tiles, uint32_t shares, hipStream_t stream) {
+void shrink_launch(const Adapt<T>& p, hipStream_t stream) {
     uint32_t lds = kWaves * kR * kTT * 1024 + kTT * 16 * p.rankp * 4;
     if (kBoth) lds += kTT * 16 * p.wide * 2;
     // more than 64 KB has to be asked for
@@ -614,22 +647,23 @@ void shrink_launch(const Adapt<T>& p, uint32_t tiles, uint32_t shares, hipStream
         reinterpret_cast<const void*>(&adapt_shrink<T, kBoth, kR, kTT, kWaves>),
         hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
     (void)ready;
-    adapt_shrink<T, kBoth, kR, kTT, kWaves><<<dim3(tiles, shares), kWaves * 64, lds, stream>>>(p);
+    adapt_shrink<T, kBoth, kR, kTT, kWaves><<<p.tiles * (kBoth ? p.shares : p.splits), kWaves * 64, lds, stream>>>(p);
 }
 
 template <class T, bool kBoth, int kTT, int kWaves>
-void shrink_rank(const Adapt<T>& p, uint32_t tiles, uint32_t shares, hipStream_t stream) {
+void shrink_rank(const Adapt<T>& p, hipStream_t stream) {
     if (p.rankp <= 16)
-        shrink_launch<T, kBoth, 1, kTT, kWaves>(p, tiles, shares, stream);
+        shrink_launch<T, kBoth, 1, kTT, kWaves>(p, stream);
     else if (p.rankp <= 32)
-        shrink_launch<T, kBoth, 2, kTT, kWaves>(p, tiles, shares, stream);
+        shrink_launch<T, kBoth, 2, kTT, kWaves>(p, stream);
     else
-        shrink_launch<T, kBoth, 4, kTT, kWaves>(p, tiles, shares, stream);
+        shrink_launch<T, kBoth, 4, kTT, kWaves>(p, stream);
 }
 
 template <class T, int kTok, int kTT, int kC, int kFast>
-void expand_base(const Adapt<T>& p, dim3 grid, hipStream_t stream) {
+void expand_base(const Adapt<T>& p, hipStream_t stream) {
     constexpr int kWaves = 4;
+    const uint32_t grid = (uint32_t)p.tiles * p.shares;
     if (!p.base)
         adapt_expand<T, kTok, kTT, kC, kFast, kNoBase, kWaves><<<grid, kWaves * 64, 0, stream>>>(p);
     else if (p.base_f32)
@@ -638,19 +672,23 @@ void expand_base(const Adapt<T>& p, dim3 grid, hipStream_t stream) {
         adapt_expand<T, kTok, kTT, kC, kFast, kBaseT, kWaves><<<grid, kWaves * 64, 0, stream>>>(p);
 }
 
+// Columns a workgroup and the workgroups of a tile: enough to fill the card, if
+// `tiles` tiles have rows.
+template <class T>
+void share_columns(Adapt<T>& p, int columns, int64_t tiles, int64_t wanted) {
+    const int64_t shares = std::min(groups(p.n, columns), std::max<int64_t>(1, wanted / tiles));
+    p.columns = (int32_t)(groups(groups(p.n, shares), columns) * columns);
+    p.shares = (int32_t)groups(p.n, p.columns);
+}
+
 template <class T, int kTok, int kTT, int kC>
-void expand_launch(Adapt<T> p, uint32_t grid, int64_t tiles, hipStream_t stream) {
-    constexpr int kWaves = 4, kCols = kWaves / (kTok / (kTT * 16)) * kC * 16;
-    const int64_t shares = std::min(groups(p.n, kCols), std::max<int64_t>(1, 2048 / tiles));
-    p.columns = (int32_t)(groups(groups(p.n, shares), kCols) * kCols);
-    // the columns of a tile one after another: rows whose length is a multiple of
-    // many channels' width are read along, not across
-    const dim3 by((uint32_t)groups(p.n, p.columns), grid);
+void expand_launch(Adapt<T> p, int64_t tiles, hipStream_t stream) {
+    share_columns(p, 4 / (kTok / (kTT * 16)) * kC * 16, tiles, 4096);
     const int fast = p.parts == 2 ? p.rankp : 0;
-    if (fast == 16) return expand_base<T, kTok, kTT, kC, 16>(p, by, stream);
-    if (fast == 32) return expand_base<T, kTok, kTT, kC, 32>(p, by, stream);
-    if (fast == 64) return expand_base<T, kTok, kTT, kC, 64>(p, by, stream);
-    expand_base<T, kTok, kTT, kC, 0>(p, by, stream);
+    if (fast == 16) return expand_base<T, kTok, kTT, kC, 16>(p, stream);
+    if (fast == 32) return expand_base<T, kTok, kTT, kC, 32>(p, stream);
+    if (fast == 64) return expand_base<T, kTok, kTT, kC, 64>(p, stream);
+    expand_base<T, kTok, kTT, kC, 0>(p, stream);
 }
 
 // Floats of `work` that a tile takes beside its shares of h.
@@ -669,13 +707,12 @@ void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
         grid = p.count < kCounted ? std::min<int64_t>(p.m, p.m / kTok + p.count + 1) : p.m;
         tiles = std::min<int64_t>(grid, tiles + p.count);
     }
+    p.tiles = (int32_t)grid;
     const uint64_t sums = (uint64_t)kTok * p.rankp, each = tile_floats(p, kTok);
     if (floats < grid * each) {
-        constexpr int kCols = kWaves * (kTT == 1 ? 4 : 2) * 16;
-        const int64_t shares = std::min(groups(p.n, kCols), std::max<int64_t>(1, 1024 / tiles));
-        p.columns = (int32_t)(groups(groups(p.n, shares), kCols) * kCols);
+        share_columns(p, kWaves * (kTT == 1 ? 4 : 2) * 16, tiles, 1024);
         p.splits = 1;
-        return shrink_rank<T, true, kTT, kWaves>(p, (uint32_t)grid, (uint32_t)groups(p.n, p.columns), stream);
+        return shrink_rank<T, true, kTT, kWaves>(p, stream);
     }
     // workgroups that share a tile's k: to fill the card, each wave left with
     // two rounds of loads or more
@@ -688,8 +725,8 @@ void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
     p.row = reinterpret_cast<int32_t*>(p.factor + grid * kTok);
     p.id = p.row + grid * kTok;
     p.partial = reinterpret_cast<float*>(p.id + grid * kTok);
-    shrink_rank<T, false, kTT, kWaves>(p, (uint32_t)grid, p.splits, stream);
-    expand_launch<T, kTok, kTT == 1 ? 1 : 2, 4>(p, (uint32_t)grid, tiles, stream);
+    shrink_rank<T, false, kTT, kWaves>(p, stream);
+    expand_launch<T, kTok, kTT == 1 ? 1 : 2, 4>(p, tiles, stream);
 }
 
 template <class T>
@@ -698,9 +735,6 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
     const bool many = a.m > kGathered && a.rank <= 128;
     const auto words = [](const void* at, int64_t s) {
         return reinterpret_cast<uintptr_t>(at) % 16 == 0 && s % 8 == 0;
-    };
-    const auto quad = [](const void* at, int64_t s, int size) {
-        return !at || (reinterpret_cast<uintptr_t>(at) % (4 * size) == 0 && s % 4 == 0);
     };
     p.a = static_cast<const T*>(a.a);
     p.b = static_cast<const T*>(a.b);
@@ -725,7 +759,8 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
     p.wide = (int32_t)groups(p.parts * p.rankp, 32) * 32;
     p.words = a.k % 8 == 0 && words(a.x, p.x_stride) && words(a.a, p.a_stride) && words(a.a, p.a_row);
     p.b_words = words(a.b, p.b_stride) && words(a.b, p.b_row);
-    p.quads = quad(a.out, p.out_stride, p.out_f32 ? 4 : 2) && quad(a.base, p.base_stride, p.base_f32 ? 4 : 2);
+    p.words_out = words(a.out, p.out_stride * (p.out_f32 ? 2 : 1)) &&
+                  (!a.base || words(a.base, p.base_stride * (p.base_f32 ? 2 : 1)));
     uint64_t floats = 0;
     if (a.work_bytes > kWorkHead)
         floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
@@ -745,7 +780,7 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
         if (many)
             tiles_launch<T, 2, 4>(p, static_cast<char*>(a.work), floats, stream);
         else
-            tiles_launch<T, 1, 8>(p, static_cast<char*>(a.work), floats, stream);
+            tiles_launch<T, 1, 4>(p, static_cast<char*>(a.work), floats, stream);
     }
     return launched("ii_adapt");
 }

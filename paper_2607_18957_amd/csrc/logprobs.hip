@@ -8,10 +8,14 @@
 // its order above and its token's complement below, so that no two are alike and
 // the order of arrival does not show.
 //
-// The likeliest tokens: of a tile's 256 largest keys, one a thread, the top-th is
-// a bound that `top` tokens reach, and at most `top` threads hold tokens that do.
-// Those go into a list in LDS; later tiles add what is above the list's top-th,
-// which few are. A list is cut to `top` by counting, for each, those above it.
+// The likeliest tokens: of the largest logits of a wave's 64 threads, in order, the
+// top-th is a bound that `top` tokens reach, and so is the least of the waves'
+// (top / 4)-th. What reaches the larger bound, little more than `top` tokens of a
+// tile, goes into a list in LDS; later tiles add what is above the list's top-th,
+// which few are. Where many logits are alike a bound of keys takes its place: the
+// top-th of the 256 threads' largest, of which at most `top` threads hold tokens
+// that reach it. A list is cut to `top` by counting, for each key, those above it,
+// after a bound of the same kind has left few.
 //
 // Bound by memory; for 16-bit logits the vector units are close behind.
 #include <algorithm>
@@ -84,11 +88,13 @@ __device__ inline Sums shuffled(const Sums& a, int d) {
 // The order of floats in whole numbers (-0 as +0; NaN as -infinity), above the
 // complement of the token, so that of equal logits the lower token is larger.
 // No key is 0.
+__device__ inline uint32_t order_of(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
 __device__ inline uint64_t key_of(float x, int token) {
     if (!(x == x)) x = -INFINITY;
-    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
-    const uint32_t order = b & 0x80000000u ? ~b : b | 0x80000000u;
-    return (uint64_t)order << 32 | (uint32_t)~token;
+    return (uint64_t)order_of(x) << 32 | (uint32_t)~token;
 }
 __device__ inline float logit_of(uint64_t key) {
     const uint32_t order = (uint32_t)(key >> 32);
@@ -99,7 +105,8 @@ struct List {
     uint64_t key[kList];
     uint64_t sorted[II_MAX_TOP];
     uint64_t best[kThreads], least;  // of a tile
-    uint32_t count, added[3], again;
+    uint32_t count, added[3], more, again;
+    float room[2][kThreads / 64];
 };
 
 // How many of the n keys are above mine. n is even, or key[n] is 0.
@@ -114,11 +121,67 @@ __device__ inline int above(const uint64_t* key, int n, uint64_t mine) {
     return c;
 }
 
+// A bound that `top` of the threads' values `mine` reach: the largest of the
+// waves' top-th ones, or the least of the waves' (top / 4)-th, whichever is
+// larger. Called by all threads; `room` is free before and after.
+__device__ inline float bound_of(float mine, int top, float (&room)[2][kThreads / 64]) {
+    const int lane = threadIdx.x % 64;
+    // the wave's values in falling order, by exchanges of two sorted halves
+#pragma unroll
+    for (int k = 2; k <= 64; k *= 2)
+#pragma unroll
+        for (int d = k / 2; d > 0; d /= 2) {
+            const float other = __shfl_xor(mine, d);
+            const bool larger = ((lane & k) == 0) == ((lane & d) == 0);
+            mine = larger ? fmaxf(mine, other) : fminf(mine, other);
+        }
+    constexpr int kWaves = kThreads / 64;
+    const float one = __shfl(mine, top - 1), all = __shfl(mine, (top + kWaves - 1) / kWaves - 1);
+    __syncthreads();
+    if (lane == 0) {
+        room[0][threadIdx.x / 64] = one;
+        room[1][threadIdx.x / 64] = all;
+    }
+    __syncthreads();
+    float most = room[0][0], least = room[1][0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+        most = fmaxf(most, room[0][w]);
+        least = fminf(least, room[1][w]);
+    }
+    return fmaxf(most, least);
+}
+
 // Cuts the list to its `top` largest keys, in order. Called by all threads with
 // what was written before them in place; they may read the list after it. Keys
 // of 0, which may be many, come last.
 __device__ inline void prune(List& l, int top) {
-    const int n = (int)l.count;
+    __syncthreads();
+    int n = (int)l.count;
+    if (n > 2 * II_MAX_TOP) {
+        // only what reaches a bound of the threads' largest can be among them
+        constexpr int kEach = kList / kThreads;
+        uint64_t mine[kEach], best = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = i * kThreads + threadIdx.x;
+            mine[i] = at < n ? l.key[at] : 0;
+            best = max(best, mine[i]);
+        }
+        const uint32_t bound = order_of(bound_of(best ? logit_of(best) : -INFINITY, top, l.room));
+        int hits = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) hits += mine[i] && (uint32_t)(mine[i] >> 32) >= bound;
+        if (threadIdx.x == 0) l.again = 0;
+        __syncthreads();
+        uint32_t place = 0;
+        if (hits) place = atomicAdd(&l.again, (uint32_t)hits);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (mine[i] && (uint32_t)(mine[i] >> 32) >= bound) l.key[place++] = mine[i];
+        __syncthreads();
+        n = (int)l.again;
+    }
     if (threadIdx.x < II_MAX_TOP) l.sorted[threadIdx.x] = 0;
     if (threadIdx.x == 0 && n % 2) l.key[n] = 0;
     __syncthreads();
@@ -207,10 +270,15 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                 const int top = p.top;
                 // a token as good as the bound's comes after it and is not above it
                 const auto real = [&](int i) { return whole || (at(i) >= lead && at(i) < end); };
-                const bool full = (int)list.count >= top;
+                if ((int)list.count < top) {
+                    // what reaches the bound is above a key that no token has
+                    const float reach = bound_of(most == most ? most : -INFINITY, top, list.room);
+                    if (reach > -INFINITY) bound = max(bound, (uint64_t)order_of(reach) << 32);
+                }
+                const bool full = bound != 0;
                 const float least = logit_of(bound);
                 int hits = 0;
-                if (!full || most > least)
+                if (!full || most >= least)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         hits += real(i) && key_of(x[i], (int)(at(i) - lead)) > bound;
@@ -232,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                         list.best[t] = mine;
                         if (t == 0) {
                             list.least = 0;
-                            list.again = 0;
+                            list.more = 0;
                         }
                         __syncthreads();
                         if (mine && above(list.best, kThreads, mine) == top - 1) list.least = mine;
@@ -243,9 +311,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
                             hits += real(i) && key_of(x[i], (int)(at(i) - lead)) > bound;
-                        if (hits) place = atomicAdd(&list.again, (uint32_t)hits);
+                        if (hits) place = atomicAdd(&list.more, (uint32_t)hits);
                         __syncthreads();
-                        added = list.again;
+                        added = list.more;
                     }
                     place += list.count;
                     if (hits)
