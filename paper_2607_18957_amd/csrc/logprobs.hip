@@ -28,7 +28,9 @@ namespace ii {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kList = 2048;       // keys a list holds
+constexpr int kEach = 32;         // logits of a tile a thread
+constexpr int kTile = kThreads * kEach;
+constexpr int kList = 2560;       // keys a list holds
 constexpr int kPruned = 256;      // and how many beyond 3 top are put up with
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -77,12 +79,25 @@ __device__ inline void join(Sums& a, Sums b, float scale) {
     a.t += b.t;
 }
 
-__device__ inline Sums shuffled(const Sums& a, int d) {
-    Sums b;
-    b.m = __shfl_xor(a.m, d);
-    b.s = __shfl_xor(a.s, d);
-    b.t = __shfl_xor(a.t, d);
-    return b;
+// Those of the workgroup's threads: their maximum, then all relative to it, in the
+// order of lanes and waves. Called by all threads.
+__device__ inline Sums sum_of(Sums a, float scale, Sums (&waves)[kThreads / 64]) {
+    float most = a.m;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    move_to(a, most, scale);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        a.s += __shfl_xor(a.s, d);
+        a.t += __shfl_xor(a.t, d);
+    }
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = a;
+    __syncthreads();
+    a = waves[0];
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) join(a, waves[w], scale);
+    return a;
 }
 
 // The order of floats in whole numbers (-0 as +0; NaN as -infinity), above the
@@ -96,10 +111,10 @@ __device__ inline uint64_t key_of(float x, int token) {
     if (!(x == x)) x = -INFINITY;
     return (uint64_t)order_of(x) << 32 | (uint32_t)~token;
 }
-__device__ inline float logit_of(uint64_t key) {
-    const uint32_t order = (uint32_t)(key >> 32);
+__device__ inline float float_of(uint32_t order) {
     return __builtin_bit_cast(float, order & 0x80000000u ? order & 0x7fffffffu : ~order);
 }
+__device__ inline float logit_of(uint64_t key) { return float_of((uint32_t)(key >> 32)); }
 
 struct List {
     uint64_t key[kList];
@@ -204,9 +219,8 @@ struct Word {  // 16 bytes of logits
 
 template <class T, bool kTop>
 __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
-    constexpr int kWord = Word<T>::size, kWords = 16 / kWord;  // 16 logits a thread and tile
-    constexpr int kTile = kThreads * 16;
-    static_assert(II_MAX_TOP * 16 + II_MAX_TOP < kList - 1);
+    constexpr int kWord = Word<T>::size, kWords = kEach / kWord;
+    static_assert(II_MAX_TOP * kEach + II_MAX_TOP < kList - 1);
     using vec = __attribute__((ext_vector_type(kWord))) T;
     __shared__ __attribute__((aligned(16))) char lds[kTop ? sizeof(List) : 16];
     __shared__ Sums waves[kThreads / 64];
@@ -230,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
         }
         int turn = 0;  // of three counters: one in use, one read, one cleared
         for (int64_t base = begin; base < end; base += kTile) {
-            float x[16];
+            float x[kEach];
             const auto at = [&](int i) { return base + ((int64_t)(i / kWord) * kThreads + t) * kWord + i % kWord; };
             const bool whole = base >= lead && base + kTile <= end;
             if (whole) {
@@ -254,12 +268,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
             }
             float most = x[0];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) most = fmaxf(most, x[i]);
+            for (int i = 1; i < kEach; ++i) most = fmaxf(most, x[i]);
             move_to(sums, fmaxf(sums.m, most), p.scale);
             const float ref = sums.m == -INFINITY ? 0.0f : sums.m;
             float s = 0, below = 0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < kEach; ++i) {
                 const float d = x[i] - ref, e = exp2_of(d * to2);
                 s += e;
                 below = fmaf(e, fmaxf(d, -3e38f), below);
@@ -268,20 +282,24 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
             sums.t += below;
             if constexpr (kTop) {
                 const int top = p.top;
-                // a token as good as the bound's comes after it and is not above it
                 const auto real = [&](int i) { return whole || (at(i) >= lead && at(i) < end); };
                 if ((int)list.count < top) {
-                    // what reaches the bound is above a key that no token has
                     const float reach = bound_of(most == most ? most : -INFINITY, top, list.room);
+                    // below the keys of what reaches it
                     if (reach > -INFINITY) bound = max(bound, (uint64_t)order_of(reach) << 32);
                 }
-                const bool full = bound != 0;
-                const float least = logit_of(bound);
-                int hits = 0;
-                if (!full || most >= least)
+                // Logits from here on are above the bound: of those that equal a
+                // token's the later ones are not. Without a bound all are.
+                const float from_here = float_of((uint32_t)(bound >> 32) + ((uint32_t)bound != 0));
+                uint32_t mask = 0;
+                if (bound) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        hits += real(i) && key_of(x[i], (int)(at(i) - lead)) > bound;
+                    for (int i = 0; i < kEach; ++i) mask |= (x[i] >= from_here ? 1u : 0u) << i;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) mask |= (real(i) ? 1u : 0u) << i;
+                }
+                int hits = __popc(mask);
                 uint32_t place = 0;
                 if (hits) place = atomicAdd(&list.added[turn], (uint32_t)hits);
                 __syncthreads();
@@ -295,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                         // `top` threads hold any
                         uint64_t mine = 0;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
+                        for (int i = 0; i < kEach; ++i)
                             if (real(i)) mine = max(mine, key_of(x[i], (int)(at(i) - lead)));
                         list.best[t] = mine;
                         if (t == 0) {
@@ -307,10 +325,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                         __syncthreads();
                         if (list.least) bound = max(bound, list.least - 1);
                         prune(list, top);
-                        hits = 0;
+                        mask = 0;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            hits += real(i) && key_of(x[i], (int)(at(i) - lead)) > bound;
+                        for (int i = 0; i < kEach; ++i)
+                            mask |= (real(i) && key_of(x[i], (int)(at(i) - lead)) > bound ? 1u : 0u) << i;
+                        hits = __popc(mask);
                         if (hits) place = atomicAdd(&list.more, (uint32_t)hits);
                         __syncthreads();
                         added = list.more;
@@ -318,10 +337,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                     place += list.count;
                     if (hits)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const uint64_t k = key_of(x[i], (int)(at(i) - lead));
-                            if (real(i) && k > bound) list.key[place++] = k;
-                        }
+                        for (int i = 0; i < kEach; ++i)
+                            if (mask >> i & 1) list.key[place++] = key_of(x[i], (int)(at(i) - lead));
                     __syncthreads();
                     if (t == 0) list.count += added;
                     __syncthreads();
@@ -333,20 +350,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
             }
         }
 
-        // the sums of the workgroup, in the order of its waves
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            // both lanes of a pair join the lower one's to the upper one's
-            const Sums o = shuffled(sums, d);
-            Sums a = t & d ? o : sums;
-            join(a, t & d ? sums : o, p.scale);
-            sums = a;
-        }
-        if (t % 64 == 0) waves[t / 64] = sums;
-        __syncthreads();
-        sums = waves[0];
-#pragma unroll
-        for (int w = 1; w < kThreads / 64; ++w) join(sums, waves[w], p.scale);
+        sums = sum_of(sums, p.scale, waves);
         if constexpr (kTop) {
             if (p.parts == 1 || (int)list.count > p.top) prune(list, p.top);
         }
@@ -371,7 +375,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                 }
             if (!arrive_last(&p.counters[row], p.parts)) continue;
             sums = no_sums();
-            for (int q = 0; q < p.parts; ++q) {
+            for (int q = t; q < p.parts; q += kThreads) {
                 const f32x4 m = take_part(parts, q * p.room * 4);
                 const f64x2 st = __builtin_bit_cast(f64x2, take_part(parts, q * p.room * 4 + 16));
                 Sums b;
@@ -380,6 +384,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                 b.t = st[1];
                 join(sums, b, p.scale);
             }
+            sums = sum_of(sums, p.scale, waves);
             if constexpr (kTop) {
                 // as many parts at once as the list has room for beside `top`
                 const int pairs = (p.top + 1) / 2, step = max(1, (kList - 2 - p.top) / (2 * pairs));
@@ -447,18 +452,18 @@ int run(const ii_logprobs_args& a, hipStream_t stream) {
     p.counters = nullptr;
     p.partial = nullptr;
     // few rows are cut into parts of a tile or more
-    constexpr int64_t kTile = kThreads * 16, kWanted = 1024;
+    constexpr int64_t kWanted = 768;
     int64_t parts = 1;
     if (a.work_bytes > kWorkHead && a.rows <= (int64_t)kWorkCounters) {
         p.counters = static_cast<uint32_t*>(a.work);
         p.partial = reinterpret_cast<float*>(static_cast<char*>(a.work) + kWorkHead);
         const int64_t floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
-        parts = std::min({groups(a.vocab, kTile), kWanted / a.rows, floats / (a.rows * p.room)});
+        parts = std::min<int64_t>({groups(a.vocab, kTile), kWanted / a.rows, floats / (a.rows * p.room)});
         if (a.top) parts = std::min<int64_t>(parts, 1024 / a.top);
         parts = std::max<int64_t>(parts, 1);
     }
     // a row may begin inside a word
-    p.part = (int32_t)(groups(groups(a.vocab + 7, parts), kTile / 16) * (kTile / 16));
+    p.part = (int32_t)(groups(groups(a.vocab + 7, parts), kThreads) * kThreads);
     p.parts = (int32_t)groups(a.vocab + 7, p.part);
     const dim3 grid(p.parts, (uint32_t)std::min<int64_t>(a.rows, 65535));
     if (a.top)
