@@ -269,14 +269,12 @@ enum {
  *   magnitude * (a cos t - b sin t),  magnitude * (b cos t + a sin t),
  *   t = position * freqs[i],
  *
- * the elements from rot_dim on stay. Angles, sines and products are held in 64
- * bits, so that far positions keep their angle and every result is the
- * definition's, rounded once.
+ * the elements from rot_dim on stay. Angles and sines are held in 64 bits, so that
+ * far positions keep their angle, products in 32, those of keys that are
+ * quantised in 64; each result is rounded once.
  *
- *   positions  of each token; any, though past 2^31 the angle is right to
- *              2^-22 only.
- *   freqs      rot_dim / 2 frequencies in radians, at most 2^10 in magnitude
- *              (ii_rotary_freqs).
+ *   positions  of each token; any whose angles are below 2^50 radians.
+ *   freqs      rot_dim / 2 frequencies in radians a position (ii_rotary_freqs).
  *   rot_dim    even, 0 to the heads' dim.
  *   magnitude  finite.
  */

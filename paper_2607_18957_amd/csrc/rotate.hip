@@ -6,11 +6,12 @@
 // pass through it, each in dim / 8 lanes of 8 elements, which find the other
 // halves of their pairs in LDS or beside them.
 //
-// Angles and products are held in 64 bits, which run at the rate of 32 here: the
-// angle of a far position would lose its last digits, and a key would be rounded
-// to the wrong 8-bit code where it lies next to the middle of two. The way from
-// 64 bits to a result is one rounding: through a float whose last bit remembers
-// what was cut off (round_odd).
+// Angles and sines are held in 64 bits: the angle of a far position would lose its
+// last digits. Products of 32 bits are enough for results of 16, but a key that is
+// quantised would be rounded to the wrong code where it lies next to the middle of
+// two, so its products are held in 64 bits too, which run at the rate of 32 here;
+// the way from there is one rounding, through a float whose last bit remembers what
+// was cut off (round_odd).
 //
 // Bound by memory.
 #include <algorithm>
@@ -39,6 +40,7 @@ struct Rotate {
 };
 
 constexpr int kWaves = 4;
+constexpr int kAhead = 4;  // rounds whose loads are on their way
 
 // cos and sin of position * freq: the product in two doubles, whole turns taken
 // off it with 2 pi in two doubles.
@@ -69,137 +71,184 @@ __device__ inline void wave_meets() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Heads 0 .. q.heads - 1 are q's; with kAppend those of keys and of values
-// follow, which go to the cache.
+// Bytes of LDS of a wave.
+__host__ __device__ constexpr int lds_of(int rot, bool quant) {
+    return 1024 + (rot / 2 + rot / 2 % 2) * 8 + (quant ? rot * 8 : 0);
+}
+
+// Rounds of as many heads as a wave holds: those of q, then with kAppend those of
+// keys and of values, which go to the cache.
 template <class T, bool kAppend, bool kQuant>
 __global__ __launch_bounds__(kWaves * 64) void rotate_heads(Rotate p, Heads q, Heads k, Heads v,
                                                             CacheAt c) {
     using x8 = typename Vec<T>::x8;
+    using f32x2 = __attribute__((ext_vector_type(2))) float;
+    using f64x2 = __attribute__((ext_vector_type(2))) double;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x % 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int pairs = p.rot / 2;
-    using f64x2 = __attribute__((ext_vector_type(2))) double;
-    f64x2* turns = reinterpret_cast<f64x2*>(lds + wave * (pairs * 16 + 1024));
-    T* room = reinterpret_cast<T*>(turns + pairs);
+    // sines in 64 bits if keys are quantised, in 32, and a wave's heads
+    char* const at = lds + wave * lds_of(p.rot, kQuant);
+    T* room = reinterpret_cast<T*>(at);
+    f32x2* turns = reinterpret_cast<f32x2*>(at + 1024);
+    f64x2* turns64 = reinterpret_cast<f64x2*>(at + 1024 + pairs * 8 + pairs % 2 * 8);
 
     const int mine = lane / p.lanes, first = lane % p.lanes * 8;  // head, its first element here
     const bool used = mine < p.at_once;
-    const bool turned = first < p.rot;
     const bool halves = p.layout == II_ROTARY_HALF;
-    const int total = q.heads + (kAppend ? 2 * k.heads : 0);
-    const int step = p.at_once * p.splits;
+    // where the others of this lane's pairs are, and its own sines
+    const T* head = room + (used ? mine * p.lanes * 8 : 0);
+    const bool words = pairs % 8 == 0;
+    const int across = first >= p.rot ? first : first < pairs ? first + pairs : first - pairs;
+    const auto sines = [&](auto* from, int j) {
+        const int e = first + j;
+        auto t = from[halves ? (e < pairs ? e : e - pairs) : e / 2];
+        if (halves ? e < pairs : j % 2 == 0) t[1] = -t[1];
+        return t;
+    };
+    const auto others = [&](u32x4 raw) {
+        const x8 x = __builtin_bit_cast(x8, raw);
+        x8 o;
+        if (halves) {
+            *reinterpret_cast<u32x4*>(room + lane * 8) = raw;
+            wave_meets();
+            if (words) {
+                o = *reinterpret_cast<const x8*>(head + across);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int e = first + j;
+                    o[j] = head[e >= p.rot ? e : e < pairs ? e + pairs : e - pairs];
+                }
+            }
+            wave_meets();  // read before the next head's are written
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = x[j ^ 1];
+        }
+        return o;
+    };
+
+    const int q_rounds = (q.heads + p.at_once - 1) / p.at_once;
+    const int kv_rounds = kAppend ? (k.heads + p.at_once - 1) / p.at_once : 0;
+    const int rounds = q_rounds + 2 * kv_rounds;
     const int64_t units = p.tokens * p.splits;
     for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < units;
          unit += (int64_t)gridDim.x * kWaves) {
         const int64_t token = unit / p.splits;
-        int base = (int)(unit - token * p.splits) * p.at_once;
+        int round = (int)(unit - token * p.splits);
         int64_t slot = -1;
         if (kAppend) slot = p.slots[token];
         const int64_t page = slot >> c.page_bits;
         const bool kept = kAppend && slot >= 0 && page < c.pages;
         const int64_t row = slot & (((int64_t)1 << c.page_bits) - 1);
 
-        const auto load = [&](int h) {
+        const auto load = [&](int r) {
             u32x4 x = {};
-            if (!used || h >= total) return x;
             const uint8_t* from;
-            if (!kAppend || h < q.heads)
+            int h = r * p.at_once + mine;
+            if (!kAppend || r < q_rounds) {
+                if (r >= rounds || !used || h >= q.heads) return x;
                 from = q.x + token * q.x_token + h * q.x_head;
-            else if (!kept)
-                return x;
-            else if (h < q.heads + k.heads)
-                from = k.x + token * k.x_token + (h - q.heads) * k.x_head;
-            else
-                from = v.x + token * v.x_token + (h - q.heads - k.heads) * v.x_head;
+            } else {
+                h -= q_rounds * p.at_once;
+                const bool of_k = r < q_rounds + kv_rounds;
+                if (!of_k) h -= kv_rounds * p.at_once;
+                if (r >= rounds || !used || !kept || h >= k.heads) return x;
+                if (of_k)
+                    from = k.x + token * k.x_token + h * k.x_head;
+                else
+                    from = v.x + token * v.x_token + h * v.x_head;
+            }
             return *reinterpret_cast<const u32x4*>(from + first * 2);
         };
-        u32x4 next = load(base + mine);
+        u32x4 ahead[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) ahead[i] = load(round + i * p.splits);
 
         const double position = (double)p.positions[token];
         for (int i = lane; i < pairs; i += 64) {
             double co, si;
             turn_of(position, p.freqs[i], &co, &si);
-            turns[i] = f64x2{co * p.magnitude, si * p.magnitude};
+            co *= p.magnitude;
+            si *= p.magnitude;
+            turns[i] = f32x2{(float)co, (float)si};
+            if (kQuant) turns64[i] = f64x2{co, si};
         }
         wave_meets();
-        double co[8], si[8];
+        float co[8], si[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int e = first + j;
             co[j] = 1;
             si[j] = 0;
-            if (e < p.rot) {
-                const f64x2 t = turns[halves ? (e < pairs ? e : e - pairs) : e / 2];
+            if (first + j < p.rot) {
+                const f32x2 t = sines(turns, j);
                 co[j] = t[0];
-                si[j] = (halves ? e < pairs : j % 2 == 0) ? -t[1] : t[1];
+                si[j] = t[1];
             }
         }
 
-        for (; base < total; base += step) {
-            const int h = base + mine;
-            const u32x4 raw = next;
-            next = load(h + step);
+        const auto pass = [&](u32x4 raw) {
             const x8 x = __builtin_bit_cast(x8, raw);
-            // the others of the pairs
-            x8 o;
-            if (halves) {
-                *reinterpret_cast<u32x4*>(room + lane * 8) = raw;
-                wave_meets();
-                const T* head = room + (used ? mine * p.lanes * 8 : 0);
-                if (pairs % 8 == 0) {
-                    const int e = first < pairs ? first + pairs : first - pairs;
-                    o = *reinterpret_cast<const x8*>(head + (turned ? e : first));
-                } else {
+            const bool of_q = round < q_rounds, of_k = round < q_rounds + kv_rounds;
+            x8 y = x;
+            if (of_q || (of_k && !kQuant)) {
+                const x8 o = others(raw);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float t = fmaf((float)x[j], co[j], (float)o[j] * si[j]);
+                    y[j] = first + j < p.rot ? (T)t : x[j];
+                }
+            }
+            if (!kAppend || of_q) {
+                const int h = round * p.at_once + mine;
+                if (used && h < q.heads)
+                    *reinterpret_cast<x8*>(q.out + token * q.out_token + h * q.out_head + first * 2) = y;
+                return;
+            }
+            const int h = (round - q_rounds - (of_k ? 0 : kv_rounds)) * p.at_once + mine;
+            const bool put = used && kept && h < k.heads;
+            uint8_t* to = (of_k ? c.at[0] : c.at[1]) + page * c.page_stride + h * c.head_stride +
+                          row * c.token_stride;
+            if constexpr (kQuant) {
+                float z[8];
+                if (of_k) {
+                    const x8 o = others(raw);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int e = first + j;
-                        o[j] = head[e >= p.rot ? e : e < pairs ? e + pairs : e - pairs];
+                        z[j] = (float)x[j];
+                        if (first + j < p.rot) {
+                            const f64x2 t = sines(turns64, j);
+                            z[j] = round_odd(fma((double)z[j], t[0], (double)(float)o[j] * t[1]));
+                        }
                     }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) z[j] = (float)x[j];
                 }
-                wave_meets();  // read before the next head's are written
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = x[j ^ 1];
-            }
-            const bool value = kAppend && h >= q.heads + k.heads;
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const double t = fma((double)(float)x[j], co[j], (double)(float)o[j] * si[j]);
-                y[j] = value || first + j >= p.rot ? (float)x[j] : round_odd(t);
-            }
-            if (!kAppend || h < q.heads) {
-                if (used && h < total) {
-                    x8 out;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) out[j] = (T)y[j];
-                    *reinterpret_cast<x8*>(q.out + token * q.out_token + h * q.out_head + first * 2) = out;
-                }
-            }
-            if constexpr (kAppend) {
                 // four neighbouring lanes hold a block, of one head
-                uint32_t exponent = 0;
-                u32x2 code = {};
-                if (kQuant) code = quantise<T>(y, &exponent);
-                if (used && kept && h >= q.heads && h < total) {
-                    const int kh = value ? h - q.heads - k.heads : h - q.heads;
-                    const int64_t at = page * c.page_stride + kh * c.head_stride + row * c.token_stride;
-                    uint8_t* to = (value ? c.at[1] : c.at[0]) + at;
-                    if (kQuant) {
-                        *reinterpret_cast<u32x2*>(to + first) = code;
-                        if (first % 32 == 0)
-                            (value ? c.scale[1] : c.scale[0])[page * c.scale_page_stride +
-                                                              kh * c.scale_head_stride +
-                                                              row * c.scale_token_stride + first / 32] =
-                                (uint8_t)exponent;
-                    } else {
-                        x8 out;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) out[j] = value ? x[j] : (T)y[j];
-                        *reinterpret_cast<x8*>(to + first * 2) = out;
-                    }
+                uint32_t exponent;
+                const u32x2 code = quantise<T>(z, &exponent);
+                if (put) {
+                    *reinterpret_cast<u32x2*>(to + first) = code;
+                    if (first % 32 == 0)
+                        (of_k ? c.scale[0] : c.scale[1])[page * c.scale_page_stride +
+                                                         h * c.scale_head_stride +
+                                                         row * c.scale_token_stride + first / 32] =
+                            (uint8_t)exponent;
                 }
+            } else if (put) {
+                *reinterpret_cast<x8*>(to + first * 2) = y;
+            }
+        };
+        while (round < rounds) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i, round += p.splits) {
+                if (round >= rounds) break;
+                const u32x4 raw = ahead[i];
+                ahead[i] = load(round + kAhead * p.splits);
+                pass(raw);
             }
         }
         wave_meets();  // sines read before the next token's are written
@@ -219,7 +268,7 @@ Heads heads_of(const ii_turn& t) {
 }
 
 // How `heads` heads of each token are given to waves.
-dim3 shape(Rotate* p, const ii_rotary& r, int64_t tokens, int64_t heads, int dim) {
+dim3 shape(Rotate* p, const ii_rotary& r, int64_t tokens, int64_t q_heads, int64_t kv_heads, int dim) {
     p->positions = r.positions;
     p->freqs = r.freqs;
     p->magnitude = r.magnitude;
@@ -229,7 +278,7 @@ dim3 shape(Rotate* p, const ii_rotary& r, int64_t tokens, int64_t heads, int dim
     p->lanes = dim / 8;
     p->at_once = 64 / p->lanes;
     // enough waves to fill the card, though each forms its token's sines again
-    const int64_t rounds = groups(heads, p->at_once);
+    const int64_t rounds = groups(q_heads, p->at_once) + 2 * groups(kv_heads, p->at_once);
     p->splits = (int32_t)std::max<int64_t>(1, std::min(rounds, 4096 / std::max<int64_t>(tokens, 1)));
     return dim3((uint32_t)std::min<int64_t>(groups(tokens * p->splits, kWaves), 1 << 20));
 }
@@ -272,9 +321,9 @@ int check_turn(const char* fn, const ii_turn& t, Rows* x, Rows* out) {
 template <class T>
 void turn(const ii_turn& t, const ii_rotary& r, hipStream_t stream) {
     Rotate p = {};
-    const dim3 grid = shape(&p, r, t.tokens, t.heads, t.dim);
+    const dim3 grid = shape(&p, r, t.tokens, t.heads, 0, t.dim);
     const Heads h = heads_of(t);
-    rotate_heads<T, false, false><<<grid, kWaves * 64, kWaves * (p.rot * 8 + 1024), stream>>>(
+    rotate_heads<T, false, false><<<grid, kWaves * 64, kWaves * lds_of(p.rot, false), stream>>>(
         p, h, Heads{}, Heads{}, CacheAt{});
 }
 
@@ -303,14 +352,15 @@ void put(const ii_cache& c, const ii_tokens& f, const ii_rotary& r, const ii_tur
          hipStream_t stream) {
     Rotate p = {};
     const Heads h = q ? heads_of(*q) : Heads{};
-    const dim3 grid = shape(&p, r, f.tokens, h.heads + 2 * (int64_t)c.heads, c.dim);
+    const dim3 grid = shape(&p, r, f.tokens, h.heads, c.heads, c.dim);
     p.slots = f.slots;
     const Heads k = {static_cast<const uint8_t*>(f.k), nullptr, f.k_token_stride * 2,
                      f.k_head_stride * 2, 0, 0, c.heads};
     const Heads v = {static_cast<const uint8_t*>(f.v), nullptr, f.v_token_stride * 2,
                      f.v_head_stride * 2, 0, 0, c.heads};
-    const uint32_t lds = kWaves * (p.rot * 8 + 1024);
-    if (c.dtype == II_FP8_E4M3)
+    const bool quant = c.dtype == II_FP8_E4M3;
+    const uint32_t lds = kWaves * lds_of(p.rot, quant);
+    if (quant)
         rotate_heads<T, true, true><<<grid, kWaves * 64, lds, stream>>>(p, h, k, v, cache_at(c));
     else
         rotate_heads<T, true, false><<<grid, kWaves * 64, lds, stream>>>(p, h, k, v, cache_at(c));

@@ -70,9 +70,11 @@ def turn(x, positions, freqs, layout="half", magnitude=1.0):
 
 def rounded(y, dtype):
     """Bound of a turned value that is rounded to dtype once: angles of up to
-    2^24 radians are off by 2^-28, sines by as much."""
+    2^24 radians are off by 2^-28, sines by as much. The sines are rounded to
+    float, one product is, and their sum: 3 E of |x cos| + |o sin|, which is at
+    most |x| + |o| <= 2 max(|y|, |y'|) over a pair's two results."""
     size = y.abs().amax(-1, keepdim=True) * 2
-    return y.abs() * U[dtype] * (1 + 2 * E) + size * 2.0 ** -27 + TINY[dtype]
+    return y.abs() * U[dtype] * (1 + 2 * E) + size * (2.0 ** -27 + 3 * E) + TINY[dtype]
 
 
 def kept(y, f16=False):
