@@ -53,6 +53,7 @@ struct Adapt {
     T* held;              // [wide]
     float* factor;        // of a result
     int32_t *row, *id;    // -1: none
+    int32_t* used;        // rows of A, columns of B
 };
 
 template <class T>
@@ -65,11 +66,16 @@ __device__ inline int rank_of(const Adapt<T>& p, int a) {
     return p.ranks ? min(max(p.ranks[a], 0), p.rank) : p.rank;
 }
 
+template <class T>
+__device__ inline float scale_of(const Adapt<T>& p, int a) {
+    return p.scales ? p.scales[a] : 1.0f;
+}
+
 // A tile's rows and their adapters, -1 for none; places past the last row have
 // row -1.
 template <int kTok>
 struct Tile {
-    int row[kTok], id[kTok];
+    int row[kTok], id[kTok], rank[kTok];
     float factor[kTok];  // of a result
 };
 
@@ -98,7 +104,8 @@ __device__ inline bool gather(const Adapt<T>& p, int t, Tile<kTok>& tile) {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
         const int j = i * 64 + lane;
-        id[i] = j < p.m ? adapter_of(p, j) : -2;
+        id[i] = -2;
+        if (j < p.m) id[i] = adapter_of(p, j);
     }
     int mine = -2, from = 0;  // the tile's adapter; its rows from this one on
     if (p.count < kCounted) {
@@ -107,7 +114,8 @@ __device__ inline bool gather(const Adapt<T>& p, int t, Tile<kTok>& tile) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kWords; ++i)
-            if (i % (blockDim.x / 64) == threadIdx.x / 64 && id[i] >= -1) atomicAdd(&rows[id[i] + 1], 1);
+            if (i * 64 < p.m && i % (blockDim.x / 64) == threadIdx.x / 64 && id[i] >= -1)
+                atomicAdd(&rows[id[i] + 1], 1);
         __syncthreads();
         int before = 0;
         for (int c0 = 0; c0 <= p.count && mine == -2; c0 += 64) {
@@ -139,9 +147,13 @@ __device__ inline bool gather(const Adapt<T>& p, int t, Tile<kTok>& tile) {
         }
         if (from % kTok) return false;
     }
+    // asked for here, wanted later
+    const int rank = mine < 0 ? 0 : rank_of(p, mine);
+    const float factor = mine < 0 ? 0.0f : scale_of(p, mine);
     int found = 0;
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
+        if (i * 64 >= p.m) break;
         const uint64_t same = __ballot(id[i] == mine);
         const int place = found + __popcll(same & ((1ull << lane) - 1)) - from;
         if (threadIdx.x < 64 && same >> lane & 1 && place >= 0 && place < kTok) {
@@ -154,6 +166,10 @@ __device__ inline bool gather(const Adapt<T>& p, int t, Tile<kTok>& tile) {
         tile.row[threadIdx.x] = -1;
         tile.id[threadIdx.x] = -1;
     }
+    if (threadIdx.x < kTok) {
+        tile.rank[threadIdx.x] = rank;
+        tile.factor[threadIdx.x] = factor;
+    }
     __syncthreads();
     return true;
 }
@@ -164,20 +180,26 @@ __device__ inline void neighbours(const Adapt<T>& p, int b, Tile<kTok>& tile) {
     if (threadIdx.x < kTok) {
         const int64_t i = (int64_t)b * kTok + threadIdx.x;
         tile.row[threadIdx.x] = i < p.m ? (int)i : -1;
-        tile.id[threadIdx.x] = i < p.m ? adapter_of(p, i) : -1;
+        const int id = i < p.m ? adapter_of(p, i) : -1;
+        tile.id[threadIdx.x] = id;
+        tile.rank[threadIdx.x] = id < 0 ? 0 : rank_of(p, id);
+        tile.factor[threadIdx.x] = id < 0 ? 0.0f : scale_of(p, id);
     }
     __syncthreads();
 }
 
-// The least adapter of the tile above a, or INT_MAX.
+// The least adapter of the tile above a, or INT_MAX; its rank.
 template <int kTok>
-__device__ inline int next_adapter(const Tile<kTok>& tile, int a) {
+__device__ inline int next_adapter(const Tile<kTok>& tile, int a, int& rank) {
     static_assert(kTok <= 64);
     const int id = tile.id[threadIdx.x % kTok];
     int v = id > a ? id : INT32_MAX;
 #pragma unroll
     for (int d = 1; d < kTok; d *= 2) v = min(v, __shfl_xor(v, d));
-    return __builtin_amdgcn_readfirstlane(v);
+    v = __builtin_amdgcn_readfirstlane(v);
+    const uint64_t here = __ballot(id == v);
+    rank = here ? __builtin_amdgcn_readfirstlane(tile.rank[__builtin_ctzll(here) % kTok]) : 0;
+    return v;
 }
 
 // Elements of a row from `from` on, of which `left` are there, others zero.
@@ -194,13 +216,12 @@ __device__ inline typename Vec<T>::x8 some(const T* from, int64_t left, bool wor
 // Rows r0 .. r0 + kR * 16 of h of the tile's rows whose adapter is a, this
 // workgroup's share of k, given to keep(token, rank, value).
 template <class T, int kR, int kTT, int kWaves, class Keep>
-__device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int a, int r0, int split,
+__device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int a, int rank, int r0, int split,
                               float* red, Keep&& keep) {
     using x8 = typename Vec<T>::x8;
     constexpr int kSums = kR * kTT * 256;
     const int lane = threadIdx.x % 64, row = lane % 16, part = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int rank = rank_of(p, a);
     const T *ap[kR], *xp[kTT];
 #pragma unroll
     for (int r = 0; r < kR; ++r)  // rows past the rank are left out below
@@ -293,8 +314,7 @@ __device__ inline void cut(const Adapt<T>& p, Tile<kTok>& tile, const float* h, 
                 down = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
             }
         }
-        const int id = tile.id[token];
-        if (lane == 0) tile.factor[token] = id < 0 ? 0.0f : up * (p.scales ? p.scales[id] : 1.0f);
+        if (lane == 0) tile.factor[token] *= up;
         T* to = parts + token * p.wide;
         for (int r = lane; r < p.rankp; r += kLanes) {
             float rest = mine[r] * down;
@@ -380,14 +400,14 @@ __device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 low,
 
 // Columns first, first + step, .. below end, kC * 16 at a time, of the kTT * 16
 // rows of out that a wave has: of each 16, lane l has row l mod 16, of which
-// `rows`, `ids` and `factors` are told, and `parts` is h cut, [row][wide]. kFast:
+// `rows`, `ids`, `ranks` and `factors` are told, and `parts` is h cut, [row][wide]. kFast:
 // rankp, if a row's parts are two and stay in registers (0: neither).
 //
 // Of two products of 16 columns a lane gets four columns each; the rows of B are
 // given to them so that these are eight neighbours, a word of out.
 template <class T, int kTT, int kC, int kFast, int kBase>
 __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const int (&ids)[kTT],
-                              const float (&factors)[kTT], const T* parts, int64_t first, int64_t step,
+                              const int (&ranks)[kTT], const float (&factors)[kTT], const T* parts, int64_t first, int64_t step,
                               int64_t end) {
     using x8 = typename Vec<T>::x8;
     const int lane = threadIdx.x % 64, row = lane % 16, part = lane / 16;
@@ -409,6 +429,14 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
 #pragma unroll
         for (int d = 1; d < 16; d *= 2) v = min(v, __shfl_xor(v, d));
         return __builtin_amdgcn_readfirstlane(v);
+    };
+    const auto rank_in = [&](int a) {
+        int r = 0;
+#pragma unroll
+        for (int t = 0; t < kTT; ++t)
+            if (const uint64_t here = __ballot(ids[t] == a))
+                r = __builtin_amdgcn_readlane(ranks[t], __builtin_ctzll(here));
+        return r;
     };
     // base is asked for a step ahead, behind what is read of B; alike in all
     // lanes, so that no branch comes between the loads
@@ -441,7 +469,7 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
         bool asked = false;
         f32x4 total[kC][kTT] = {};
         for (int a = a0; a != INT32_MAX; a = next(a)) {
-            const int rank = rank_of(p, a);
+            const int rank = rank_in(a);
             const T* b[kC];
 #pragma unroll
             for (int c = 0; c < kC; ++c)
@@ -563,18 +591,20 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
     const int sums = kTok * p.rankp;
     for (int e = threadIdx.x; e < sums; e += kThreads) h[e] = 0;
     __syncthreads();
-    for (int a = next_adapter(tile, -1); a != INT32_MAX; a = next_adapter(tile, a))
+    int rank;
+    for (int a = next_adapter(tile, -1, rank); a != INT32_MAX; a = next_adapter(tile, a, rank))
         for (int r0 = 0; r0 < p.rankp; r0 += kR * 16)
-            shrink<T, kR, kTT, kWaves>(p, tile, a, r0, kBoth ? 0 : mine.share, red,
+            shrink<T, kR, kTT, kWaves>(p, tile, a, rank, r0, kBoth ? 0 : mine.share, red,
                                        [&](int token, int r, float v) { h[token * p.rankp + r] = v; });
     if constexpr (kBoth) {
         T* parts = reinterpret_cast<T*>(h + sums);
         cut<T, kTok, kThreads>(p, tile, h, parts);
         const int row = threadIdx.x % 16;
-        int rows[kTT], ids[kTT];
+        int rows[kTT], ids[kTT], ranks[kTT];
         float factors[kTT];
 #pragma unroll
         for (int t = 0; t < kTT; ++t) {
+            ranks[t] = tile.rank[t * 16 + row];
             rows[t] = tile.row[t * 16 + row];
             ids[t] = tile.id[t * 16 + row];
             factors[t] = tile.factor[t * 16 + row];
@@ -584,11 +614,11 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
         const int64_t from = at + threadIdx.x / 64 * kC * 16, end = min(at + p.columns, (int64_t)p.n);
         constexpr int kStep = kWaves * kC * 16;
         if (!p.base)
-            expand<T, kTT, kC, 0, kNoBase>(p, rows, ids, factors, parts, from, kStep, end);
+            expand<T, kTT, kC, 0, kNoBase>(p, rows, ids, ranks, factors, parts, from, kStep, end);
         else if (p.base_f32)
-            expand<T, kTT, kC, 0, kBaseF32>(p, rows, ids, factors, parts, from, kStep, end);
+            expand<T, kTT, kC, 0, kBaseF32>(p, rows, ids, ranks, factors, parts, from, kStep, end);
         else
-            expand<T, kTT, kC, 0, kBaseT>(p, rows, ids, factors, parts, from, kStep, end);
+            expand<T, kTT, kC, 0, kBaseT>(p, rows, ids, ranks, factors, parts, from, kStep, end);
     } else {
         if (p.splits > 1) {
             const Rsrc parts = buffer(p.partial + (int64_t)mine.tile * p.splits * sums,
@@ -608,6 +638,7 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
         if (threadIdx.x < kTok) {
             p.row[first + threadIdx.x] = tile.row[threadIdx.x];
             p.id[first + threadIdx.x] = tile.id[threadIdx.x];
+            p.used[first + threadIdx.x] = tile.rank[threadIdx.x];
             p.factor[first + threadIdx.x] = tile.factor[threadIdx.x];
         }
     }
@@ -621,19 +652,21 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_expand(Adapt<T> p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = threadIdx.x % 16;
     const Share mine = share_of_columns(p.shares);
     const int64_t first = (int64_t)mine.tile * kTok + wave % kSides * kTT * 16;
-    int rows[kTT], ids[kTT];
+    int rows[kTT], ids[kTT], ranks[kTT];
     float factors[kTT];
     bool any = false;
 #pragma unroll
     for (int t = 0; t < kTT; ++t) {
+        // a tile without rows leaves the others as they were
         rows[t] = p.row[first + t * 16 + row];
-        ids[t] = rows[t] < 0 ? -1 : p.id[first + t * 16 + row];
-        factors[t] = ids[t] < 0 ? 0.0f : p.factor[first + t * 16 + row];
+        ids[t] = p.id[first + t * 16 + row];
+        ranks[t] = p.used[first + t * 16 + row];
+        factors[t] = p.factor[first + t * 16 + row];
         any |= rows[t] >= 0;
     }
     if (!__any(any)) return;
     const int64_t at = (int64_t)mine.share * p.columns;
-    expand<T, kTT, kC, kFast, kBase>(p, rows, ids, factors, p.held + first * p.wide,
+    expand<T, kTT, kC, kFast, kBase>(p, rows, ids, ranks, factors, p.held + first * p.wide,
                                      at + wave / kSides * kC * 16, kSteps * kC * 16,
                                      min(at + p.columns, (int64_t)p.n));
 }
@@ -694,7 +727,7 @@ void expand_launch(Adapt<T> p, int64_t tiles, hipStream_t stream) {
 // Floats of `work` that a tile takes beside its shares of h.
 template <class T>
 uint64_t tile_floats(const Adapt<T>& p, int rows) {
-    return rows * (p.wide / 2 + 3);
+    return rows * (p.wide / 2 + 4);
 }
 
 // Rows [0, p.m) of a call; floats: the room in `work`.
@@ -724,7 +757,8 @@ void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
     p.factor = reinterpret_cast<float*>(p.held + grid * kTok * p.wide);
     p.row = reinterpret_cast<int32_t*>(p.factor + grid * kTok);
     p.id = p.row + grid * kTok;
-    p.partial = reinterpret_cast<float*>(p.id + grid * kTok);
+    p.used = p.id + grid * kTok;
+    p.partial = reinterpret_cast<float*>(p.used + grid * kTok);
     shrink_rank<T, false, kTT, kWaves>(p, stream);
     expand_launch<T, kTok, kTT == 1 ? 1 : 2, 4>(p, tiles, stream);
 }
