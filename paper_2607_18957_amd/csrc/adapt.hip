@@ -230,8 +230,11 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
     for (int t = 0; t < kTT; ++t) xp[t] = p.x + max(tile.row[t * 16 + row], 0) * p.x_stride + part * 8;
     f32x4 acc[kR][kTT] = {};
     const int units = (int)groups(p.k, kUnit), whole = p.words ? p.k / kUnit : 0;
-    const int step = kWaves * p.splits;
-    int u = split * kWaves + wave;
+    // each wave takes neighbouring units: rows begin at few of the memory's
+    // channels, and waves side by side would be at the same ones
+    const int each = (units + kWaves * p.splits - 1) / (kWaves * p.splits);
+    const int begin = (split * kWaves + wave) * each;
+    const int end = min(begin + each, units), full = min(end, whole);
     constexpr int kAhead = kTT > 1 ? 2 : 4;  // units whose loads are on their way
     const auto take = [&](int u, x8(&av)[2][kR], x8(&xv)[2][kTT]) {
 #pragma unroll
@@ -252,18 +255,17 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
                 for (int t = 0; t < kTT; ++t) acc[r][t] = mfma16(av[h][r], xv[h][t], acc[r][t]);
     };
     if (rank > r0) {
-        for (; u < whole; u += kAhead * step) {
+        for (int u = begin; u < full; u += kAhead) {
             x8 av[kAhead][2][kR], xv[kAhead][2][kTT];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i)
-                if (u + i * step < whole) take(u + i * step, av[i], xv[i]);
+                if (u + i < full) take(u + i, av[i], xv[i]);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i)
-                if (u + i * step < whole) multiply(av[i], xv[i]);
+                if (u + i < full) multiply(av[i], xv[i]);
         }
         // what is left, past the last whole unit
-        while (u - step >= whole) u -= step;
-        for (; u < units; u += step) {
+        for (int u = max(begin, whole); u < end; ++u) {
             x8 av[2][kR], xv[2][kTT];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -568,6 +570,12 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
     }
 }
 
+template <bool kBoth, int kR, int kTT, int kWaves, class T>
+__host__ __device__ inline int first_lds(const Adapt<T>& p) {
+    const int red = kWaves * kR * kTT * 1024, parts = kBoth ? kTT * 16 * p.wide * 2 : 0;
+    return red > parts ? red : parts;
+}
+
 // h of a tile, cut: in LDS, formed by each of the workgroups that share
 // the tile's columns, which follow (kBoth); or in memory, by the last to arrive of
 // those that share k.
@@ -586,8 +594,9 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
     } else {
         neighbours(p, mine.tile, tile);
     }
+    // what waves add up, and h cut after it, in one place; h
     float* red = reinterpret_cast<float*>(lds);
-    float* h = red + kWaves * kR * kTT * 256;
+    float* h = reinterpret_cast<float*>(lds + first_lds<kBoth, kR, kTT, kWaves>(p));
     const int sums = kTok * p.rankp;
     for (int e = threadIdx.x; e < sums; e += kThreads) h[e] = 0;
     __syncthreads();
@@ -597,7 +606,7 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
             shrink<T, kR, kTT, kWaves>(p, tile, a, rank, r0, kBoth ? 0 : mine.share, red,
                                        [&](int token, int r, float v) { h[token * p.rankp + r] = v; });
     if constexpr (kBoth) {
-        T* parts = reinterpret_cast<T*>(h + sums);
+        T* parts = reinterpret_cast<T*>(lds);
         cut<T, kTok, kThreads>(p, tile, h, parts);
         const int row = threadIdx.x % 16;
         int rows[kTT], ids[kTT], ranks[kTT];
@@ -673,13 +682,8 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_expand(Adapt<T> p) {
 
 template <class T, bool kBoth, int kR, int kTT, int kWaves>
 void shrink_launch(const Adapt<T>& p, hipStream_t stream) {
-    uint32_t lds = kWaves * kR * kTT * 1024 + kTT * 16 * p.rankp * 4;
-    if (kBoth) lds += kTT * 16 * p.wide * 2;
-    // more than 64 KB has to be asked for
-    static const hipError_t ready = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(&adapt_shrink<T, kBoth, kR, kTT, kWaves>),
-        hipFuncAttributeMaxDynamicSharedMemorySize, 150 * 1024);
-    (void)ready;
+    // at most 48 KB
+    const uint32_t lds = first_lds<kBoth, kR, kTT, kWaves>(p) + kTT * 16 * p.rankp * 4;
     adapt_shrink<T, kBoth, kR, kTT, kWaves><<<p.tiles * (kBoth ? p.shares : p.splits), kWaves * 64, lds, stream>>>(p);
 }
 
@@ -799,7 +803,8 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
     if (a.work_bytes > kWorkHead)
         floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
     // rows that are gathered, or whose tiles there is room for, at once
-    int64_t rows = many ? a.m : std::min<int64_t>(a.m, kGathered);
+    // (a dispatch counts its work-items in 32 bits)
+    int64_t rows = std::min<int64_t>(a.m, many ? 1 << 20 : kGathered);
     if (many && floats >= tile_floats(p, 32))
         rows = std::min<int64_t>(rows, floats / tile_floats(p, 32) * 32);
     for (int64_t i = 0; i < a.m; i += rows) {
