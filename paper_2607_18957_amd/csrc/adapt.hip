@@ -18,6 +18,12 @@
 // A first kernel leaves the parts and the tiles' rows in `work`, a second one
 // forms the columns of out, in waves that share nothing and never wait for one
 // another. Without `work` each workgroup of a tile's columns forms h again, in LDS.
+//
+// Many rows are bound by memory: 4099 x 4096 x 14336 with 8 adapters of rank 64 and
+// a base of 32 bits 119 us, the second kernel 90 of them at 3.9 TB/s. Few are bound
+// by the steps from one kernel's first load to the other's last store: 250 x 14336 x
+// 4096 with 32 adapters of rank 16 20 us, 4 x 4096 x 4096 12, a call's cost on the
+// host being 10.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,7 +34,9 @@ namespace ii {
 namespace {
 
 constexpr int kMaxRank = 256;
-constexpr int kGathered = 1024;  // rows that are gathered
+// Rows that are gathered: 1000 rows of 32 adapters in no order take 27 us, as
+// neighbours 91 (4096 x 4096, rank 16); in runs of 500, rank 64, 36 against 25.
+constexpr int kGathered = 1024;
 constexpr int kCounted = 1024;   // adapters (and none) whose rows are counted
 constexpr int kUnit = 64;        // elements of k a wave takes at once
 

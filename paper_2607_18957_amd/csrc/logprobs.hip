@@ -17,7 +17,10 @@
 // that reach it. A list is cut to `top` by counting, for each key, those above it,
 // after a bound of the same kind has left few.
 //
-// Bound by memory; for 16-bit logits the vector units are close behind.
+// Bound by memory: 2047 x 128256 in bf16 100 us, 5.2 TB/s, where a logit takes some
+// ten vector instructions, of which the exponential counts for four. Few rows are
+// bound by the steps from a load to the last part's joining: 48 x 128256 with the 20
+// likeliest 22 us, 1 x 8192 with 5 of them 8.6.
 #include <algorithm>
 #include <cmath>
 
@@ -28,7 +31,8 @@ namespace ii {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kEach = 32;         // logits of a tile a thread
+// Logits of a tile a thread: with 16, 2047 x 128256 took 106 us, 1 x 8192 11.4.
+constexpr int kEach = 32;
 constexpr int kTile = kThreads * kEach;
 constexpr int kList = 2560;       // keys a list holds
 constexpr int kPruned = 256;      // and how many beyond 3 top are put up with
@@ -451,7 +455,9 @@ int run(const ii_logprobs_args& a, hipStream_t stream) {
     p.room = (uint32_t)groups(8 + 2 * a.top, 4) * 4;
     p.counters = nullptr;
     p.partial = nullptr;
-    // few rows are cut into parts of a tile or more
+    // few rows are cut into parts of a tile or more, three workgroups a compute
+    // unit: with four, which wait for one another, 48 x 128256 took 31.7 us
+    // against 27.5, with two 28.0
     constexpr int64_t kWanted = 768;
     int64_t parts = 1;
     if (a.work_bytes > kWorkHead && a.rows <= (int64_t)kWorkCounters) {

@@ -7,7 +7,9 @@
 // both sides, and the additions cost nothing beside the memory. The norm before
 // the next block takes the stream as it was before its rounding.
 //
-// Bound by memory.
+// Bound by memory: 16384 x 8192, normalised before and after, with a gate for each
+// element and a stream of 32 bits, 331 us, 5.7 TB/s; a copy of 2 GiB reaches 4.9.
+// Rows of 1001, read by the element, 3.0 TB/s.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -46,7 +48,7 @@ __device__ inline void anew(float& x) { asm volatile("" : "+v"(x)); }
 template <int kThreads>
 __device__ inline double row_sum(double v, int turn) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    for (int d = 1; d < std::min(kThreads, 64); d *= 2) v += __shfl_xor(v, d);
     if constexpr (kThreads > 64) {
         __shared__ double part[2][kThreads / 64];
         if (threadIdx.x % 64 == 0) part[turn % 2][threadIdx.x / 64] = v;
@@ -63,7 +65,9 @@ __device__ inline double row_sum(double v, int turn) {
 template <class T, class S, int kThreads, int kWords, bool kWide, bool kLayer>
 __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void norm_rows(Norm<T, S> p) {
     constexpr int kBlock = kThreads > 256 ? kThreads : 256, kRows = kBlock / kThreads;
-    static_assert(kRows == 1 || kThreads == 64);
+    // several rows a wave: addresses of their own, whole words only
+    constexpr bool kPart = kThreads < 64;
+    static_assert((kRows == 1 || kThreads <= 64) && (!kPart || (kWide && kWords == 1)));
     const int t = threadIdx.x % kThreads;
     // a thread's first element, and how far the others are from it
     const int first = kWide ? t * 8 : t;
@@ -74,8 +78,14 @@ __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void norm_rows(Nor
     // row's end and leave out what would be written there.
     const auto get = [&](auto* from, int w) {
         using V = std::remove_const_t<std::remove_pointer_t<decltype(from)>>;
-        const Rsrc row = buffer(from, (int64_t)p.n * (int)sizeof(V));
         Eight<V> v;
+        if constexpr (kPart) {
+#pragma unroll
+            for (int h = 0; h < (int)sizeof(v) / 16; ++h)
+                v.word[h] = first < p.n ? reinterpret_cast<const u32x4*>(from + first)[h] : u32x4{};
+            return v;
+        }
+        const Rsrc row = buffer(from, (int64_t)p.n * (int)sizeof(V));
         if constexpr (kWide) {
 #pragma unroll
             for (int h = 0; h < (int)sizeof(v) / 16; ++h)
@@ -95,10 +105,16 @@ __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void norm_rows(Nor
     };
     const auto put = [&](auto* to, int w, const float (&from)[8]) {
         using V = std::remove_pointer_t<decltype(to)>;
-        const Rsrc row = buffer(to, (int64_t)p.n * (int)sizeof(V));
         Eight<V> v;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v.at[j] = (V)from[j];
+        if constexpr (kPart) {
+#pragma unroll
+            for (int h = 0; h < (int)sizeof(v) / 16; ++h)
+                if (first < p.n) reinterpret_cast<u32x4*>(to + first)[h] = v.word[h];
+            return;
+        }
+        const Rsrc row = buffer(to, (int64_t)p.n * (int)sizeof(V));
         if constexpr (kWide) {
 #pragma unroll
             for (int h = 0; h < (int)sizeof(v) / 16; ++h)
@@ -167,7 +183,8 @@ __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void norm_rows(Nor
         }
     };
 
-    const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);  // alike in a wave
+    int mine = threadIdx.x / kThreads;
+    if (!kPart) mine = __builtin_amdgcn_readfirstlane(mine);  // alike in a wave
     for (int64_t i = (int64_t)blockIdx.x * kRows + mine; i < p.m; i += (int64_t)gridDim.x * kRows) {
         // all loads are on their way before the first sum
         Eight<T> x[kWords], g[kWords];
@@ -209,24 +226,35 @@ void rows_launch(const Norm<T, S>& p, bool wide, hipStream_t stream) {
     // a dispatch counts its work-items in 32 bits
     const uint32_t grid = (uint32_t)std::min<int64_t>(groups(p.m, kBlock / kThreads), 1 << 21);
     const bool layer = p.kind == II_NORM_LAYER;
-    if (wide && layer)
-        norm_rows<T, S, kThreads, kWords, true, true><<<grid, kBlock, 0, stream>>>(p);
-    else if (wide)
-        norm_rows<T, S, kThreads, kWords, true, false><<<grid, kBlock, 0, stream>>>(p);
-    else if (layer)
-        norm_rows<T, S, kThreads, kWords, false, true><<<grid, kBlock, 0, stream>>>(p);
-    else
-        norm_rows<T, S, kThreads, kWords, false, false><<<grid, kBlock, 0, stream>>>(p);
+    if (wide) {
+        if (layer)
+            norm_rows<T, S, kThreads, kWords, true, true><<<grid, kBlock, 0, stream>>>(p);
+        else
+            norm_rows<T, S, kThreads, kWords, true, false><<<grid, kBlock, 0, stream>>>(p);
+    } else if constexpr (kThreads >= 64) {
+        if (layer)
+            norm_rows<T, S, kThreads, kWords, false, true><<<grid, kBlock, 0, stream>>>(p);
+        else
+            norm_rows<T, S, kThreads, kWords, false, false><<<grid, kBlock, 0, stream>>>(p);
+    }
 }
 
 template <class T, class S>
 void launch(const Norm<T, S>& p, bool wide, hipStream_t stream) {
+    // Words of a row in as few threads as keep the loads of a row apart from the
+    // next's, for some words each where that hides more: 16384 x 4096 with a
+    // residual 91 us by 512 threads against 96 by 256 of two words, 16384 x 8192
+    // normalised twice 333 by 256 of four against 338 by 512 of two, 2049 x 32768
+    // 110 by 1024 of four against 120 by 512 of eight. Short rows share a wave:
+    // 65536 x 128 13 us against 25 with a wave each.
+    if (wide && p.n <= 128) return rows_launch<T, S, 16, 1>(p, wide, stream);
+    if (wide && p.n <= 256) return rows_launch<T, S, 32, 1>(p, wide, stream);
     if (p.n <= 512) return rows_launch<T, S, 64, 1>(p, wide, stream);
     if (p.n <= 2048) return rows_launch<T, S, 256, 1>(p, wide, stream);
-    if (p.n <= 4096) return rows_launch<T, S, 256, 2>(p, wide, stream);
+    if (p.n <= 4096) return rows_launch<T, S, 512, 1>(p, wide, stream);
     if (p.n <= 8192) return rows_launch<T, S, 256, 4>(p, wide, stream);
     if (p.n <= 16384) return rows_launch<T, S, 512, 4>(p, wide, stream);
-    rows_launch<T, S, 512, 8>(p, wide, stream);
+    rows_launch<T, S, 1024, 4>(p, wide, stream);
 }
 
 template <class T, class S>
