@@ -1,13 +1,16 @@
 """Load a model's weights with one plan and answer prompts from where they lie.
 
-    python examples/generate.py [--model tiny|llama8b] [--tokens 8] [--cache fp8|bf16]
+    python examples/generate.py [--model tiny|llama8b] [--tokens 8] [--cache fp8|bf16] [--fused] [--top 3]
 
 The weights of a decoder-only transformer (synth's tables, filled with seeded
 normal values) are loaded by ii_load into one arena; every matrix is then used
 there, in place, by the operators of paper_2607_18957_amd.ops: ii_linear for
 all products (with the gate, the activation and the residual stream in their
 epilogues), ii_cache_write for new keys and values, ii_attend for prompts of
-different lengths at once, then for single tokens.
+different lengths at once, then for single tokens. With --fused the norms are
+ii_norm's and positions are turned on the way into the cache by ii_cache_append,
+in place of torch's; with --top ii_logprobs names the likeliest tokens beside each
+answer.
 """
 from __future__ import annotations
 
@@ -50,7 +53,8 @@ class Model:
     of up to `max_len` tokens."""
 
     def __init__(self, weights, meta, dim: int, seqs: int, max_len: int, page: int = 64,
-                 cache_dtype=torch.float8_e4m3fn):
+                 cache_dtype=torch.float8_e4m3fn, fused: bool = False):
+        self.fused = fused
         self.w, self.layers, self.dim = weights, meta["layers"], dim
         self.heads, self.kv_heads = meta["hidden"] // dim, meta["kv"] // dim
         self.page, self.max_len, columns = page, max_len, -(-max_len // page)
@@ -64,6 +68,7 @@ class Model:
         angle = torch.arange(max_len, device="cuda")[:, None] * 10000.0 ** (
             -torch.arange(0, dim, 2, device="cuda") / dim)
         self.turn = torch.polar(torch.ones_like(angle), angle)
+        self.freqs = ops.ii_rotary_freqs(dim)
 
     def linear(self, x, name, n, **kw):
         out = torch.empty(x.shape[0], n, dtype=kw.pop("out", x.dtype), device="cuda")
@@ -71,6 +76,10 @@ class Model:
         return out
 
     def norm(self, x, name):
+        if self.fused:
+            out = torch.empty_like(x)
+            ops.ii_norm(out, x, self.w[name], stream=torch.cuda.current_stream())
+            return out
         y = x.float()
         return (y * torch.rsqrt(y.square().mean(-1, keepdim=True) + 1e-5) * self.w[name]).to(x.dtype)
 
@@ -102,8 +111,12 @@ class Model:
             h = self.norm(x, p + "attn_norm")
             q, k, v = (self.linear(h, p + m, c * self.dim).unflatten(1, (c, self.dim)) for m, c in
                        (("q", self.heads), ("k", self.kv_heads), ("v", self.kv_heads)))
-            q, k = self.rotate(q, at), self.rotate(k, at)
-            ops.ii_cache_write(cache, k, v, slots, stream=stream)
+            if self.fused:
+                ops.ii_cache_append(cache, k, v, slots, at, self.freqs, q=q, q_out=q, layout="interleaved",
+                                    stream=stream)
+            else:
+                q, k = self.rotate(q, at), self.rotate(k, at)
+                ops.ii_cache_write(cache, k, v, slots, stream=stream)
             out = torch.empty_like(q)
             ops.ii_attend(out, q, cache, self.pages, self.lengths, start, max_q=max(counts),
                           max_len=self.max_len, work=self.work, stream=stream)
@@ -115,30 +128,47 @@ class Model:
         return self.linear(last, "lm_head", self.w["lm_head"].shape[0], out=torch.float32)
 
 
+    def likeliest(self, logits, top: int):
+        """(tokens, their log-probabilities) of each row, [rows, top]."""
+        ids = torch.empty(logits.shape[0], top, dtype=torch.int64, device="cuda")
+        logp = torch.empty(logits.shape[0], top, device="cuda")
+        ops.ii_logprobs(logits, top_ids=ids, top_logprobs=logp, work=self.work,
+                        stream=torch.cuda.current_stream())
+        return ids, logp
+
+
 def main() -> None:
     a = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     a.add_argument("--model", choices=["tiny", "llama8b"], default="tiny")
     a.add_argument("--tokens", type=int, default=8)
     a.add_argument("--cache", choices=["fp8", "bf16"], default="fp8")
+    a.add_argument("--fused", action="store_true")
+    a.add_argument("--top", type=int, default=0)
     a = a.parse_args()
     if a.tokens < 1:
         raise SystemExit("--tokens has to be 1 or more")
+    if not 0 <= a.top <= ops.MAX_TOP:
+        raise SystemExit(f"--top has to be 0 to {ops.MAX_TOP}")
     table = getattr(synth, a.model)()
     plan, _arena, weights = load(table, normal_blob(table))
     prompts = [[(7 * i + j) % table.meta["vocab"] for j in range(n)] for i, n in enumerate((5, 37, 300))]
     model = Model(weights, table.meta, 64 if a.model == "tiny" else 128, len(prompts), 300 + a.tokens,
-                  cache_dtype=torch.float8_e4m3fn if a.cache == "fp8" else torch.bfloat16)
+                  cache_dtype=torch.float8_e4m3fn if a.cache == "fp8" else torch.bfloat16, fused=a.fused)
     logits = model.step(torch.tensor(sum(prompts, []), device="cuda"), [len(p) for p in prompts])
-    answers = []
+    answers, beside = [], []
     for _ in range(a.tokens):
         torch.cuda.synchronize()
         t = time.perf_counter()
         answers.append(logits.argmax(-1))
+        if a.top:
+            beside.append(model.likeliest(logits, a.top))
         logits = model.step(answers[-1], [1] * len(prompts))
         torch.cuda.synchronize()
     print(f"{a.model}: last step {1e3 * (time.perf_counter() - t):.2f} ms")
-    for p, row in zip(prompts, torch.stack(answers, 1).tolist()):
+    for i, (p, row) in enumerate(zip(prompts, torch.stack(answers, 1).tolist())):
         print(f"prompt of {len(p)}: {row}")
+        for token, (ids, logp) in zip(row, beside):
+            print(f"  {token} of " + ", ".join(f"{j} ({x:.3f})" for j, x in zip(ids[i].tolist(), logp[i].tolist())))
     plan.free()
 
 
