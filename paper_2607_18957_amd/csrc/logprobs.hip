@@ -240,6 +240,13 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
         const vec* from = reinterpret_cast<const vec*>(logits - lead);
         const int64_t begin = (int64_t)blockIdx.x * p.part;
         const int64_t end = min(begin + p.part, (int64_t)p.vocab + lead);
+        // asked for here, wanted at the end
+        int64_t target = -1;
+        float logit = 0;
+        if (t == 0 && p.logprob) {
+            target = p.targets[row];
+            if (target >= 0 && target < p.vocab) logit = (float)logits[target];
+        }
         Sums sums = no_sums();
         uint64_t bound = 0;
         if (kTop) {
@@ -378,17 +385,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                                                                i + 1 < n ? list.key[i + 1] : 0}));
                 }
             if (!arrive_last(&p.counters[row], p.parts)) continue;
-            sums = no_sums();
-            for (int q = t; q < p.parts; q += kThreads) {
-                const f32x4 m = take_part(parts, q * p.room * 4);
-                const f64x2 st = __builtin_bit_cast(f64x2, take_part(parts, q * p.room * 4 + 16));
-                Sums b;
-                b.m = m[0];
-                b.s = st[0];
-                b.t = st[1];
-                join(sums, b, p.scale);
+            // the sums of part t, asked for before the keys
+            f32x4 m = {-INFINITY, 0, 0, 0}, st = {};
+            if (t < p.parts) {
+                m = take_part(parts, t * p.room * 4);
+                st = take_part(parts, t * p.room * 4 + 16);
             }
-            sums = sum_of(sums, p.scale, waves);
             if constexpr (kTop) {
                 // as many parts at once as the list has room for beside `top`
                 const int pairs = (p.top + 1) / 2, step = max(1, (kList - 2 - p.top) / (2 * pairs));
@@ -408,6 +410,16 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                     prune(list, p.top);
                 }
             }
+            sums = no_sums();
+            for (int q = t; q < p.parts; q += kThreads) {
+                if (q != t) {
+                    m = take_part(parts, q * p.room * 4);
+                    st = take_part(parts, q * p.room * 4 + 16);
+                }
+                const f64x2 both = __builtin_bit_cast(f64x2, st);
+                join(sums, Sums{m[0], both[0], both[1]}, p.scale);
+            }
+            sums = sum_of(sums, p.scale, waves);
         }
 
         // nothing but -infinity: every log-probability is -infinity, the entropy 0
@@ -418,8 +430,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
         };
         if (t == 0) {
             if (p.logprob) {
-                const int64_t target = p.targets[row];
-                p.logprob[row] = target >= 0 && target < p.vocab ? result((float)logits[target]) : 0.0f;
+                p.logprob[row] = target >= 0 && target < p.vocab ? result(logit) : 0.0f;
             }
             if (p.entropy) {
                 const double h = none ? 0.0 : logs - p.scale * (sums.t / sums.s);
