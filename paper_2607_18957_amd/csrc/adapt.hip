@@ -54,7 +54,7 @@ struct Adapt {
     int32_t columns;      // of out, a workgroup's
     int32_t tiles, splits;  // workgroups that share k of a tile
     int32_t shares;       // workgroups that share its columns
-    bool out_f32, base_f32, words, b_words, words_out;
+    bool out_f32, base_f32;
     uint32_t* counters;
     float* partial;       // [tiles][splits][rows of a tile][rankp]
     // what the first kernel leaves of each row of each tile
@@ -210,11 +210,19 @@ __device__ inline int next_adapter(const Tile<kTok>& tile, int a, int& rank) {
     return v;
 }
 
+// 16 bytes at any multiple of an element: the same instruction at every alignment.
+template <class V, class T>
+__device__ inline V word_at(const T* from) {
+    V v;
+    static_assert(sizeof(V) == 16);
+    __builtin_memcpy(&v, from, 16);
+    return v;
+}
 // Elements of a row from `from` on, of which `left` are there, others zero.
 template <class T>
-__device__ inline typename Vec<T>::x8 some(const T* from, int64_t left, bool words) {
+__device__ inline typename Vec<T>::x8 some(const T* from, int64_t left) {
     typename Vec<T>::x8 v = {};
-    if (words && left >= 8) return *reinterpret_cast<const typename Vec<T>::x8*>(from);
+    if (left >= 8) return word_at<typename Vec<T>::x8>(from);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (j < left) v[j] = from[j];
@@ -237,7 +245,7 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
 #pragma unroll
     for (int t = 0; t < kTT; ++t) xp[t] = p.x + max(tile.row[t * 16 + row], 0) * p.x_stride + part * 8;
     f32x4 acc[kR][kTT] = {};
-    const int units = (int)groups(p.k, kUnit), whole = p.words ? p.k / kUnit : 0;
+    const int units = (int)groups(p.k, kUnit), whole = p.k / kUnit;
     // each wave takes neighbouring units: rows begin at few of the memory's
     // channels, and waves side by side would be at the same ones
     const int each = (units + kWaves * p.splits - 1) / (kWaves * p.splits);
@@ -249,9 +257,9 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
         for (int h = 0; h < 2; ++h) {
             const int64_t k = (int64_t)u * kUnit + h * 32;
 #pragma unroll
-            for (int r = 0; r < kR; ++r) av[h][r] = *reinterpret_cast<const x8*>(ap[r] + k);
+            for (int r = 0; r < kR; ++r) av[h][r] = word_at<x8>(ap[r] + k);
 #pragma unroll
-            for (int t = 0; t < kTT; ++t) xv[h][t] = *reinterpret_cast<const x8*>(xp[t] + k);
+            for (int t = 0; t < kTT; ++t) xv[h][t] = word_at<x8>(xp[t] + k);
         }
     };
     const auto multiply = [&](const x8(&av)[2][kR], const x8(&xv)[2][kTT]) {
@@ -279,9 +287,9 @@ __device__ inline void shrink(const Adapt<T>& p, const Tile<kTT * 16>& tile, int
             for (int h = 0; h < 2; ++h) {
                 const int64_t k = (int64_t)u * kUnit + h * 32, left = p.k - k - part * 8;
 #pragma unroll
-                for (int r = 0; r < kR; ++r) av[h][r] = some(ap[r] + k, left, p.words);
+                for (int r = 0; r < kR; ++r) av[h][r] = some(ap[r] + k, left);
 #pragma unroll
-                for (int t = 0; t < kTT; ++t) xv[h][t] = some(xp[t] + k, left, p.words);
+                for (int t = 0; t < kTT; ++t) xv[h][t] = some(xp[t] + k, left);
             }
             multiply(av, xv);
         }
@@ -347,8 +355,8 @@ template <class T, int kBase>
 struct Base {
     u32x4 word[kBase == kBaseF32 ? 2 : 1];
 };
-// Columns j .. j + 7 of a row of base, and of out; `whole`: they are all there, and
-// words.
+// Columns j .. j + 7 of a row of base, and of out; `whole`: they are all
+// there.
 template <class T, int kBase>
 __device__ inline void base_of(const Adapt<T>& p, int64_t row, int64_t j, bool whole, Base<T, kBase>& v) {
     const int64_t at = row * p.base_stride + j;
@@ -357,7 +365,7 @@ __device__ inline void base_of(const Adapt<T>& p, int64_t row, int64_t j, bool w
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if (whole) {
-                v.word[h] = reinterpret_cast<const u32x4*>(from)[h];
+                v.word[h] = word_at<u32x4>(from + h * 4);
             } else {
                 v.word[h] = u32x4{};
 #pragma unroll
@@ -366,7 +374,8 @@ __device__ inline void base_of(const Adapt<T>& p, int64_t row, int64_t j, bool w
             }
         }
     } else if constexpr (kBase == kBaseT) {
-        v.word[0] = __builtin_bit_cast(u32x4, some(static_cast<const T*>(p.base) + at, p.n - j, whole));
+        const T* from = static_cast<const T*>(p.base) + at;
+        v.word[0] = whole ? word_at<u32x4>(from) : __builtin_bit_cast(u32x4, some(from, p.n - j));
     }
 }
 template <class T, int kBase>
@@ -386,8 +395,11 @@ __device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 low,
     if (p.out_f32) {
         float* out = static_cast<float*>(p.out) + at;
         if (whole) {
-            reinterpret_cast<f32x4*>(out)[0] = f32x4{y[0], y[1], y[2], y[3]};
-            reinterpret_cast<f32x4*>(out)[1] = f32x4{y[4], y[5], y[6], y[7]};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 v = {y[h * 4], y[h * 4 + 1], y[h * 4 + 2], y[h * 4 + 3]};
+                __builtin_memcpy(out + h * 4, &v, 16);
+            }
             return;
         }
 #pragma unroll
@@ -399,7 +411,7 @@ __device__ inline void put(const Adapt<T>& p, int64_t row, int64_t j, f32x4 low,
 #pragma unroll
         for (int r = 0; r < 8; ++r) v[r] = (T)y[r];
         if (whole) {
-            *reinterpret_cast<x8*>(out) = v;
+            __builtin_memcpy(out, &v, 16);
             return;
         }
 #pragma unroll
@@ -452,7 +464,7 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
     // lanes, so that no branch comes between the loads
     static_assert(kC % 2 == 0);
     Base<T, kBase> base[kC / 2][kTT], ahead[kC / 2][kTT];
-    const auto whole = [&](int64_t n0) { return p.words_out && n0 + kC * 16 <= p.n; };
+    const auto whole = [&](int64_t n0) { return n0 + kC * 16 <= p.n; };
     const auto ask = [&](int64_t n0) {
         if (kBase == kNoBase || n0 >= end) return;
         if (whole(n0)) {
@@ -485,7 +497,7 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
             for (int c = 0; c < kC; ++c)
                 b[c] = p.b + a * p.b_stride + min(n0 + c / 2 * 32 + place + c % 2 * 4, (int64_t)p.n - 1) * p.b_row;
             f32x4 acc[kC][kTT] = {};
-            const bool words = p.b_words && rank % 8 == 0 && rank > 0;
+            const bool words = rank % 8 == 0 && rank > 0;
             if constexpr (kFast != 0) {
                 x8 bv[kC][kSteps];
                 if (words) {
@@ -494,7 +506,7 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
 #pragma unroll
                         for (int s = 0; s < kSteps; ++s) {
                             const int col = (s * 32 + part * 8) % kFast;
-                            bv[c][s] = *reinterpret_cast<const x8*>(b[c] + (col < rank ? col : 0));
+                            bv[c][s] = word_at<x8>(b[c] + (col < rank ? col : 0));
                         }
                 } else {
 #pragma unroll
@@ -502,7 +514,7 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
 #pragma unroll
                         for (int s = 0; s < kSteps; ++s) {
                             const int col = (s * 32 + part * 8) % kFast;
-                            bv[c][s] = some(b[c] + col, rank - col, false);
+                            bv[c][s] = some(b[c] + col, rank - col);
                         }
                 }
                 if (!asked) ask(n0 + step);
@@ -529,10 +541,10 @@ __device__ inline void expand(const Adapt<T>& p, const int (&rows)[kTT], const i
                     if (words) {
 #pragma unroll
                         for (int c = 0; c < kC; ++c)
-                            bv[c] = *reinterpret_cast<const x8*>(b[c] + (there ? col : 0));
+                            bv[c] = word_at<x8>(b[c] + (there ? col : 0));
                     } else {
 #pragma unroll
-                        for (int c = 0; c < kC; ++c) bv[c] = some(b[c] + col, rank - col, false);
+                        for (int c = 0; c < kC; ++c) bv[c] = some(b[c] + col, rank - col);
                     }
 #pragma unroll
                     for (int t = 0; t < kTT; ++t)
@@ -779,14 +791,10 @@ template <class T>
 int run(const ii_adapt_args& a, hipStream_t stream) {
     Adapt<T> p = {};
     const bool many = a.m > kGathered && a.rank <= 128;
-    const auto words = [](const void* at, int64_t s) {
-        return reinterpret_cast<uintptr_t>(at) % 16 == 0 && s % 8 == 0;
-    };
     p.a = static_cast<const T*>(a.a);
     p.b = static_cast<const T*>(a.b);
     p.scales = a.scales;
     p.ranks = a.ranks;
-    // strides of axes of one place say nothing of how they can be read
     p.x_stride = a.m > 1 ? a.x_stride : 0;
     p.a_stride = a.count > 1 ? a.a_stride : 0;
     p.a_row = a.rank > 1 ? a.a_row_stride : 0;
@@ -803,10 +811,6 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
     p.base_f32 = a.base_dtype == II_F32;
     p.parts = p.out_f32 ? 3 : 2;
     p.wide = (int32_t)groups(p.parts * p.rankp, 32) * 32;
-    p.words = a.k % 8 == 0 && words(a.x, p.x_stride) && words(a.a, p.a_stride) && words(a.a, p.a_row);
-    p.b_words = words(a.b, p.b_stride) && words(a.b, p.b_row);
-    p.words_out = words(a.out, p.out_stride * (p.out_f32 ? 2 : 1)) &&
-                  (!a.base || words(a.base, p.base_stride * (p.base_f32 ? 2 : 1)));
     uint64_t floats = 0;
     if (a.work_bytes > kWorkHead)
         floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
