@@ -9,6 +9,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -21,11 +23,11 @@ SOURCES = ["plan.cpp", "scatter.hip", "runtime.hip", "ops.cpp", "linear.hip", "c
 ARCH = os.environ.get("II_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [
-    f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall",
-    "-Wl,-soname,libii.so",
+    f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
     # packed fp32 instructions are disabled for all device code built here
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
+LINK = [f"--offload-arch={ARCH}", "-fPIC", "-shared", "-Wl,-soname,libii.so"]
 
 
 def hipcc() -> str:
@@ -35,11 +37,7 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build libii.so)")
 
 
-def build(verbose: bool = False) -> str:
-    """Compile every source into libii.so (always recompiles)."""
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [hipcc(), *FLAGS, "-I", INCLUDE, "-I", CSRC, "-o", tmp,
-           *[os.path.join(CSRC, s) for s in SOURCES]]
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -49,6 +47,19 @@ def build(verbose: bool = False) -> str:
         raise RuntimeError(f"hipcc failed ({r.returncode}):\n{msgs}")
     if verbose and msgs.strip():
         print(msgs)
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every source (always recompiles; some at once) and link libii.so."""
+    tmp = LIB + f".tmp{os.getpid()}"
+    cc = hipcc()
+    with tempfile.TemporaryDirectory() as objects:
+        jobs = [(os.path.join(CSRC, s), os.path.join(objects, s + ".o")) for s in SOURCES]
+        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            for f in [pool.submit(_run, [cc, *FLAGS, "-I", INCLUDE, "-I", CSRC, "-c", "-o", o, s], verbose)
+                      for s, o in jobs]:
+                f.result()
+        _run([cc, *LINK, "-o", tmp, *[o for _, o in jobs]], verbose)
     os.replace(tmp, LIB)
     return LIB
 
