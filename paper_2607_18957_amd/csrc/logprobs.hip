@@ -51,7 +51,7 @@ struct Logprobs {
     uint32_t room;  // floats of a part in partial
 };
 
-// A sum of exponentials relative to m.
+// Sums of e^(z - m), and of (x - m) times that, x a logit. `to2` is scale / ln 2.
 struct Sums {
     float m;
     double s, t;
@@ -62,34 +62,34 @@ __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The same relative to m; m is not below a.m. Without a finite logit there is
 // nothing to move.
-__device__ inline void move_to(Sums& a, float m, float scale) {
+__device__ inline void move_to(Sums& a, float m, float to2) {
     if (a.m != m) {
         if (a.m == -INFINITY) {
             a.t = 0;
         } else {
             const float d = a.m - m;
-            const double c = exp2_of(d * scale * kLog2e);
+            const double c = exp2_of(d * to2);
             a.t = c * (a.t + a.s * fmaxf(d, -3e38f));
             a.s *= c;
         }
         a.m = m;
     }
 }
-__device__ inline void join(Sums& a, Sums b, float scale) {
+__device__ inline void join(Sums& a, Sums b, float to2) {
     const float m = fmaxf(a.m, b.m);
-    move_to(a, m, scale);
-    move_to(b, m, scale);
+    move_to(a, m, to2);
+    move_to(b, m, to2);
     a.s += b.s;
     a.t += b.t;
 }
 
 // Those of the workgroup's threads: their maximum, then all relative to it, in the
 // order of lanes and waves. Called by all threads.
-__device__ inline Sums sum_of(Sums a, float scale, Sums (&waves)[kThreads / 64]) {
+__device__ inline Sums sum_of(Sums a, float to2, Sums (&waves)[kThreads / 64]) {
     float most = a.m;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    move_to(a, most, scale);
+    move_to(a, most, to2);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         a.s += __shfl_xor(a.s, d);
@@ -100,7 +100,7 @@ __device__ inline Sums sum_of(Sums a, float scale, Sums (&waves)[kThreads / 64])
     __syncthreads();
     a = waves[0];
 #pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) join(a, waves[w], scale);
+    for (int w = 1; w < kThreads / 64; ++w) join(a, waves[w], to2);
     return a;
 }
 
@@ -222,7 +222,7 @@ struct Word {  // 16 bytes of logits
 };
 
 template <class T, bool kTop>
-__global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
+__global__ __launch_bounds__(kThreads, 3) void logprobs_rows(Logprobs p) {
     constexpr int kWord = Word<T>::size, kWords = kEach / kWord;
     static_assert(II_MAX_TOP * kEach + II_MAX_TOP < kList - 1);
     using vec = __attribute__((ext_vector_type(kWord))) T;
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
             float most = x[0];
 #pragma unroll
             for (int i = 1; i < kEach; ++i) most = fmaxf(most, x[i]);
-            move_to(sums, fmaxf(sums.m, most), p.scale);
+            move_to(sums, fmaxf(sums.m, most), to2);
             const float ref = sums.m == -INFINITY ? 0.0f : sums.m;
             float s = 0, below = 0;
 #pragma unroll
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
             }
         }
 
-        sums = sum_of(sums, p.scale, waves);
+        sums = sum_of(sums, to2, waves);
         if constexpr (kTop) {
             if (p.parts == 1 || (int)list.count > p.top) prune(list, p.top);
         }
@@ -417,14 +417,19 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                     st = take_part(parts, q * p.room * 4 + 16);
                 }
                 const f64x2 both = __builtin_bit_cast(f64x2, st);
-                join(sums, Sums{m[0], both[0], both[1]}, p.scale);
+                join(sums, Sums{m[0], both[0], both[1]}, to2);
             }
-            sums = sum_of(sums, p.scale, waves);
+            sums = sum_of(sums, to2, waves);
         }
 
         // nothing but -infinity: every log-probability is -infinity, the entropy 0
         const bool none = sums.m == -INFINITY && sums.s == 0;
-        const double logs = none ? 0.0 : log(sums.s);
+        // The exponentials were of z (1 + off), as scale / ln 2 was rounded: their
+        // sum's logarithm is off by off times the mean of z - m, the same way in
+        // every term, where other roundings cancel.
+        const double mean = none ? 0.0 : p.scale * (sums.t / sums.s);
+        const double off = (double)to2 / (p.scale * 1.4426950408889634) - 1;
+        const double logs = none ? 0.0 : log(sums.s) - off * mean;
         const auto result = [&](float x) {
             return none ? -INFINITY : (float)(((double)x - sums.m) * p.scale - logs);
         };
@@ -433,7 +438,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_rows(Logprobs p) {
                 p.logprob[row] = target >= 0 && target < p.vocab ? result(logit) : 0.0f;
             }
             if (p.entropy) {
-                const double h = none ? 0.0 : logs - p.scale * (sums.t / sums.s);
+                const double h = logs - mean;
                 p.entropy[row] = h < 0 ? 0.0f : (float)h;
             }
         }
