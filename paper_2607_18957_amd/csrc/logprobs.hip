@@ -504,6 +504,7 @@ int check(const ii_logprobs_args& a) {
         return fail(II_EINVAL, "%s: %lld rows of %lld logits", fn, (long long)a.rows,
                     (long long)a.vocab);
     if (!std::isfinite(a.scale) || !(a.scale > 0)) return fail(II_EINVAL, "%s: scale %g", fn, a.scale);
+    if (!a.rows) return II_OK;  // operands of no elements may be NULL
     if (!a.targets != !a.logprob)
         return fail(II_EINVAL, "%s: logprob and targets go together", fn);
     if (!a.top_ids != !a.top || !a.top_logprobs != !a.top)
@@ -511,7 +512,6 @@ int check(const ii_logprobs_args& a) {
     if (!a.logprob && !a.entropy && !a.top)
         return fail(II_EINVAL, "%s: nothing is wanted", fn);
     if (a.logits_stride < 0) return fail(II_EINVAL, "%s: a stride is negative", fn);
-    if (!a.rows) return II_OK;
     const uint64_t rows = a.rows, size = a.dtype == II_F32 ? 4 : 2;
     uint64_t stride;
     if (__builtin_mul_overflow((uint64_t)(rows > 1 ? a.logits_stride : 0), size, &stride))

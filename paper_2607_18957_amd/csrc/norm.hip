@@ -308,6 +308,7 @@ int check(const ii_norm_args& a) {
         return fail(II_EINVAL, "%s: %lld rows of %lld elements", fn, (long long)a.m, (long long)a.n);
     if (!std::isfinite(a.scale) || !std::isfinite(a.offset) || !std::isfinite(a.eps) || a.eps < 0)
         return fail(II_EINVAL, "%s: scale %g, eps %g, offset %g", fn, a.scale, a.eps, a.offset);
+    if (!a.m || !a.n) return II_OK;  // operands of no elements may be NULL
     if (!a.post && (a.post_weight || a.post_bias))
         return fail(II_EINVAL, "%s: post_weight or post_bias without post", fn);
     if (!a.out && (a.weight || a.bias)) return fail(II_EINVAL, "%s: weight or bias without out", fn);
@@ -317,7 +318,6 @@ int check(const ii_norm_args& a) {
     if (a.m > 1 && ((a.sum && a.sum_stride < a.n) || (a.out && a.out_stride < a.n)))
         return fail(II_EINVAL, "%s: rows of sum or out meet (strides %lld, %lld, %lld elements)", fn,
                     (long long)a.sum_stride, (long long)a.out_stride, (long long)a.n);
-    if (!a.m || !a.n) return II_OK;
     const uint64_t m = a.m, n = a.n, wide = a.stream_dtype == II_F32 ? 4 : 2;
     struct Operand {
         const char* what;

@@ -506,3 +506,22 @@ def test_refusals(work):
     _refused("II_EOVERLAP", lambda: ops.ii_logprobs(z, entropy=work.view(F32)[:4], work=work))
     many = torch.zeros(4, 65, dtype=torch.int64, device=DEV)
     _refused("II_EINVAL", lambda: ops.ii_logprobs(z, top_ids=many, top_logprobs=many.float()))
+
+
+@pytest.mark.parametrize("nbytes", [16, 65536, 65536 + 64, 65536 + 4096, 1 << 20])
+def test_logprobs_scratch(nbytes):
+    """Any size of scratch will do; its counters are left at zero."""
+    scratch = torch.zeros(nbytes, dtype=torch.uint8, device=DEV)
+    x = _normal(_gen(13), 5, 70001, dtype=F32, std=3.0)
+    for top in (0, 9, 64):
+        _check_logprobs(x, top, 1.0, scratch)
+    assert not scratch[:65536].any()
+
+
+def test_rows_of_no_elements():
+    """Nothing to write, nothing to read: no address is looked at."""
+    none = torch.empty(3, 0, dtype=BF16, device=DEV)
+    ops.ii_norm(none, none, residual=none.float(), sum=none.float())
+    ops.ii_rotate(*[torch.empty(0, 4, 64, dtype=BF16, device=DEV)] * 2, torch.empty(0, dtype=torch.int64, device=DEV),
+                  ops.ii_rotary_freqs(64))
+    ops.ii_logprobs(torch.empty(0, 100, device=DEV), entropy=torch.empty(0, device=DEV))
