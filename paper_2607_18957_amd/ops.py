@@ -82,6 +82,15 @@ def _rows(t, what: str) -> tuple[int, int]:
     return t.data_ptr(), s
 
 
+def _matrix(t, shape, dt, what: str) -> tuple[int, int]:
+    """(address, row stride) of a matrix that may be missing."""
+    if t is None:
+        return 0, 0
+    if t.shape != shape or t.dtype != dt:
+        raise ValueError(f"{what} is not {list(shape)} of {dt}")
+    return _rows(t, what)
+
+
 def _vector(t, n: int, dt, what: str) -> int:
     if t is None:
         return 0
@@ -219,21 +228,25 @@ def ii_norm(out, x, weight=None, *, bias=None, post: bool = False, post_weight=N
     """sum = scale * gate * y + residual, y = x or (post) x normalised; out = sum
     normalised. A norm is of kind "rms" or "layer", times (weight + offset), plus
     bias. out or sum may be None; sum may be residual, and out x."""
-    (m, n), dt = x.shape, x.dtype
+    shape, dt = x.shape, x.dtype
+    m, n = shape
     xp, xs = _rows(x, "x")
-    stream_dt = next((t.dtype for t in (residual, sum) if t is not None), dt)
-    at = []
-    for t, want, what in ((gate, dt, "gate"), (residual, stream_dt, "residual"), (sum, stream_dt, "sum"),
-                          (out, dt, "out")):
-        if t is None:
-            at += [0, 0]
-            continue
-        _fits(t.shape == (m, n) and t.dtype == want, f"{what} is not [m, n] of its type")
-        at += _rows(t, what)
-    vectors = [_vector(t, n, dt, w) for t, w in ((post_weight, "post_weight"), (post_bias, "post_bias"),
-                                                 (weight, "weight"), (bias, "bias"))]
-    args = _NORM.pack(_code(_CODES, dt), _code(_CODES, stream_dt), _code(NORMS, kind), bool(post), m, n, xp,
-                      xs, *at[:4], *vectors, *at[4:], scale, eps, offset, 0)
+    held = dt if residual is None and sum is None else (sum if residual is None else residual).dtype
+    gp, gs = _matrix(gate, shape, dt, "gate")
+    rp, rs = _matrix(residual, shape, held, "residual")
+    sp, ss = _matrix(sum, shape, held, "sum")
+    op, os_ = _matrix(out, shape, dt, "out")
+    pw = pb = wp = bp = 0
+    if post_weight is not None:
+        pw = _vector(post_weight, n, dt, "post_weight")
+    if post_bias is not None:
+        pb = _vector(post_bias, n, dt, "post_bias")
+    if weight is not None:
+        wp = _vector(weight, n, dt, "weight")
+    if bias is not None:
+        bp = _vector(bias, n, dt, "bias")
+    args = _NORM.pack(_code(_CODES, dt), _code(_CODES, held), _code(NORMS, kind), bool(post), m, n, xp, xs,
+                      gp, gs, rp, rs, pw, pb, wp, bp, sp, ss, op, os_, scale, eps, offset, 0)
     rc = _call_norm(args, ii._stream(stream))
     if rc:
         ii._check(rc, "ii_norm")
