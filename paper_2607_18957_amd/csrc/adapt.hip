@@ -17,7 +17,8 @@
 //
 // A first kernel leaves the parts and the tiles' rows in `work`, a second one
 // forms the columns of out, in waves that share nothing and never wait for one
-// another. Without `work` each workgroup of a tile's columns forms h again, in LDS.
+// another. Without `work`, and where the sums are short, each workgroup of a tile's
+// columns forms h again, in LDS.
 //
 // Many rows are bound by memory: 4099 x 4096 x 14336 with 8 adapters of rank 64 and
 // a base of 32 bits 119 us, the second kernel 90 of them at 3.9 TB/s. Few are bound
@@ -766,7 +767,13 @@ void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
     }
     p.tiles = (int32_t)grid;
     const uint64_t sums = (uint64_t)kTok * p.rankp, each = tile_floats(p, kTok);
-    if (floats < grid * each) {
+    // One kernel, without room for what the first leaves, or where h is formed again
+    // by every workgroup of a tile's columns in one round of loads: 1 x 512 x 1024
+    // 7.2 us against 8.3 in two (a call 9.6 against 12.0), 24 x 1024 x 1024 8.0
+    // against 10.5, 200 x 1024 x 8192 13.5 against 13.5 of rank 16; of rank 64
+    // 24 x 1024 x 8192 takes 23.1 against 17.5.
+    const bool short_sums = kTT == 1 && p.rankp <= 16 && p.k <= kUnit * 4 * kWaves;
+    if (floats < grid * each || short_sums) {
         share_columns(p, kWaves * (kTT == 1 ? 4 : 2) * 16, tiles, 1024);
         p.splits = 1;
         return shrink_rank<T, true, kTT, kWaves>(p, stream);
