@@ -3,9 +3,10 @@
 //
 // Rows of one adapter share what is read of it, so rows are taken in tiles of
 // one adapter. A few rows, in any order, are gathered: a workgroup counts the
-// rows of each adapter and finds which of them its tile of 16 has. Of many rows,
-// which come in runs, a tile is 32 neighbours, with a pass for each adapter among
-// them.
+// rows of each adapter and finds which of them its tile of 16 has. Many are put into
+// the order of their adapters first, by a kernel of one workgroup; their tiles have
+// 32. Where there are more adapters than are counted, or no `work` to note the order
+// in, a tile is 32 neighbours, with a pass for each adapter among them.
 //
 // h = A x is a sum over k that the waves of a workgroup, and workgroups, share.
 // For the product with B, whose matrix instruction takes 16 bits, a row of h is
@@ -21,7 +22,7 @@
 // columns forms h again, in LDS.
 //
 // Many rows are bound by memory: 4099 x 4096 x 14336 with 8 adapters of rank 64 and
-// a base of 32 bits 119 us, the second kernel 90 of them at 3.9 TB/s. Few are bound
+// a base of 32 bits 121 us, the second kernel 90 of them at 3.9 TB/s. Few are bound
 // by the steps from one kernel's first load to the other's last store: 250 x 14336 x
 // 4096 with 32 adapters of rank 16 20 us, 4 x 4096 x 4096 12, a call's cost on the
 // host being 10.
@@ -35,9 +36,11 @@ namespace ii {
 namespace {
 
 constexpr int kMaxRank = 256;
-// Rows that are gathered: 1000 rows of 32 adapters in no order take 27 us, as
-// neighbours 91 (4096 x 4096, rank 16); in runs of 500, rank 64, 36 against 25.
-constexpr int kGathered = 1024;
+// Rows that are gathered: 300 rows of 8 adapters take 14.6 us, put into order 17.3
+// (4096 x 4096, rank 16); 700 in runs of 350, rank 64, to 14336 39.8 against 34.4,
+// 1000 of 32 adapters in no order 26.7 against 22.3. (As neighbours 2000 of 32
+// adapters took 109 us, in order 31.)
+constexpr int kGathered = 512;
 constexpr int kCounted = 1024;   // adapters (and none) whose rows are counted
 constexpr int kUnit = 64;        // elements of k a wave takes at once
 
@@ -56,6 +59,7 @@ struct Adapt {
     int32_t tiles, splits;  // workgroups that share k of a tile
     int32_t shares;       // workgroups that share its columns
     bool out_f32, base_f32;
+    bool ordered;         // the tiles' rows are in memory before the first kernel
     uint32_t* counters;
     float* partial;       // [tiles][splits][rows of a tile][rankp]
     // what the first kernel leaves of each row of each tile
@@ -183,18 +187,88 @@ __device__ inline bool gather(const Adapt<T>& p, int t, Tile<kTok>& tile) {
     return true;
 }
 
-// Rows b kTok .. as they come.
+// Tile b of many rows, in the order that adapt_order has left, or as they come.
+// False if it has none.
 template <class T, int kTok>
-__device__ inline void neighbours(const Adapt<T>& p, int b, Tile<kTok>& tile) {
+__device__ inline bool of_many(const Adapt<T>& p, int b, Tile<kTok>& tile) {
+    if (p.ordered && p.row[(int64_t)b * kTok] < 0) return false;
     if (threadIdx.x < kTok) {
-        const int64_t i = (int64_t)b * kTok + threadIdx.x;
-        tile.row[threadIdx.x] = i < p.m ? (int)i : -1;
-        const int id = i < p.m ? adapter_of(p, i) : -1;
+        int64_t i = (int64_t)b * kTok + threadIdx.x;
+        int id = -1;
+        if (p.ordered) {
+            id = p.id[i];
+            i = p.row[i];
+        } else {
+            if (i >= p.m) i = -1;
+            if (i >= 0) id = adapter_of(p, i);
+        }
+        tile.row[threadIdx.x] = (int)i;
         tile.id[threadIdx.x] = id;
         tile.rank[threadIdx.x] = id < 0 ? 0 : rank_of(p, id);
         tile.factor[threadIdx.x] = id < 0 ? 0.0f : scale_of(p, id);
     }
     __syncthreads();
+    return true;
+}
+
+// Many rows in the order of their adapters, each adapter's from a tile's first
+// place on: places without a row have row -1. One workgroup counts, adds up and
+// puts them; rows of an adapter come in no order, which no result depends on, but
+// 64 neighbours of one stay together.
+constexpr int kOrderThreads = 1024;
+template <class T, int kTok>
+__global__ __launch_bounds__(kOrderThreads) void adapt_order(Adapt<T> p) {
+    __shared__ int rows[kCounted], next[kCounted], waves[kOrderThreads / 64];
+    const int t = threadIdx.x, lane = t % 64;
+    rows[t] = 0;
+    __syncthreads();
+    // takes a place for each lane's adapter (0: none), the lanes of one together
+    const auto take = [&](int* from, int64_t i) {
+        const int id = i < p.m ? adapter_of(p, i) + 1 : -1;
+        const int first = __builtin_amdgcn_readfirstlane(id);
+        if (__ballot(id != first) == 0) {
+            int at = 0;
+            if (lane == 0 && first >= 0) at = atomicAdd(&from[first], 64);
+            return __shfl(at, 0) + lane;
+        }
+        return id >= 0 ? atomicAdd(&from[id], 1) : 0;
+    };
+    for (int64_t i = t; i - t < p.m; i += kOrderThreads) take(rows, i);
+    __syncthreads();
+    static_assert(kCounted == kOrderThreads);
+    const int held = t <= p.count ? rows[t] : 0, tiles = (held + kTok - 1) / kTok;
+    int to = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int v = __shfl_up(to, d);
+        if (lane >= d) to += v;
+    }
+    if (lane == 63) waves[t / 64] = to;
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kOrderThreads / 64; ++w) {
+        if (w < t / 64) before += waves[w];
+        total += waves[w];
+    }
+    const int first = (before + to - tiles) * kTok;
+    next[t] = first;
+    for (int e = first + held; e < first + tiles * kTok; ++e) {
+        p.row[e] = -1;
+        p.id[e] = -1;
+    }
+    for (int64_t e = (int64_t)total * kTok + t; e < (int64_t)p.tiles * kTok; e += kOrderThreads) {
+        p.row[e] = -1;
+        p.id[e] = -1;
+    }
+    __syncthreads();
+    for (int64_t i = t; i - t < p.m; i += kOrderThreads) {
+        const int e = take(next, i);
+        if (i < p.m) {
+            p.row[e] = (int)i;
+            p.id[e] = adapter_of(p, i);
+        }
+    }
 }
 
 // The least adapter of the tile above a, or INT_MAX; its rank.
@@ -613,7 +687,7 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
             return;
         }
     } else {
-        neighbours(p, mine.tile, tile);
+        if (!of_many(p, mine.tile, tile)) return;
     }
     // what waves add up, and h cut after it, in one place; h
     float* red = reinterpret_cast<float*>(lds);
@@ -666,8 +740,10 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_shrink(Adapt<T> p) {
         }
         cut<T, kTok, kThreads>(p, tile, h, p.held + first * p.wide);
         if (threadIdx.x < kTok) {
-            p.row[first + threadIdx.x] = tile.row[threadIdx.x];
-            p.id[first + threadIdx.x] = tile.id[threadIdx.x];
+            if (!p.ordered) {
+                p.row[first + threadIdx.x] = tile.row[threadIdx.x];
+                p.id[first + threadIdx.x] = tile.id[threadIdx.x];
+            }
             p.used[first + threadIdx.x] = tile.rank[threadIdx.x];
             p.factor[first + threadIdx.x] = tile.factor[threadIdx.x];
         }
@@ -703,7 +779,7 @@ __global__ __launch_bounds__(kWaves * 64) void adapt_expand(Adapt<T> p) {
 
 template <class T, bool kBoth, int kR, int kTT, int kWaves>
 void shrink_launch(const Adapt<T>& p, hipStream_t stream) {
-    // at most 48 KB
+    // at most 56 KB
     const uint32_t lds = first_lds<kBoth, kR, kTT, kWaves>(p) + kTT * 16 * p.rankp * 4;
     adapt_shrink<T, kBoth, kR, kTT, kWaves><<<p.tiles * (kBoth ? p.shares : p.splits), kWaves * 64, lds, stream>>>(p);
 }
@@ -714,8 +790,10 @@ void shrink_rank(const Adapt<T>& p, hipStream_t stream) {
         shrink_launch<T, kBoth, 1, kTT, kWaves>(p, stream);
     else if (p.rankp <= 32)
         shrink_launch<T, kBoth, 2, kTT, kWaves>(p, stream);
-    else
+    else if (kTT == 1 || p.rankp <= 128)
         shrink_launch<T, kBoth, 4, kTT, kWaves>(p, stream);
+    else  // h leaves less room
+        shrink_launch<T, kBoth, 2, kTT, kWaves>(p, stream);
 }
 
 template <class T, int kTok, int kTT, int kC, int kFast>
@@ -761,8 +839,9 @@ void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
     constexpr int kTok = kTT * 16;
     int64_t tiles = groups(p.m, kTok);  // at least
     int64_t grid = tiles;
-    if (kTT == 1) {
-        grid = p.count < kCounted ? std::min<int64_t>(p.m, p.m / kTok + p.count + 1) : p.m;
+    const bool counted = p.count < kCounted;
+    if (kTT == 1 || counted) {
+        grid = counted ? std::min<int64_t>(p.m, p.m / kTok + p.count + 1) : p.m;
         tiles = std::min<int64_t>(grid, tiles + p.count);
     }
     p.tiles = (int32_t)grid;
@@ -774,6 +853,7 @@ void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
     // 24 x 1024 x 8192 takes 23.1 against 17.5.
     const bool short_sums = kTT == 1 && p.rankp <= 16 && p.k <= kUnit * 4 * kWaves;
     if (floats < grid * each || short_sums) {
+        if (kTT > 1) p.tiles = (int32_t)(tiles = groups(p.m, kTok));  // as they come
         share_columns(p, kWaves * (kTT == 1 ? 4 : 2) * 16, tiles, 1024);
         p.splits = 1;
         return shrink_rank<T, true, kTT, kWaves>(p, stream);
@@ -790,6 +870,10 @@ void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
     p.id = p.row + grid * kTok;
     p.used = p.id + grid * kTok;
     p.partial = reinterpret_cast<float*>(p.used + grid * kTok);
+    p.ordered = kTT > 1 && counted;
+    if constexpr (kTT > 1) {
+        if (p.ordered) adapt_order<T, kTok><<<1, kOrderThreads, 0, stream>>>(p);
+    }
     shrink_rank<T, false, kTT, kWaves>(p, stream);
     expand_launch<T, kTok, kTT == 1 ? 1 : 2, 4>(p, tiles, stream);
 }
@@ -797,7 +881,6 @@ void tiles_launch(Adapt<T> p, char* work, uint64_t floats, hipStream_t stream) {
 template <class T>
 int run(const ii_adapt_args& a, hipStream_t stream) {
     Adapt<T> p = {};
-    const bool many = a.m > kGathered && a.rank <= 128;
     p.a = static_cast<const T*>(a.a);
     p.b = static_cast<const T*>(a.b);
     p.scales = a.scales;
@@ -821,11 +904,15 @@ int run(const ii_adapt_args& a, hipStream_t stream) {
     uint64_t floats = 0;
     if (a.work_bytes > kWorkHead)
         floats = (std::min<uint64_t>(a.work_bytes, II_WORK_BYTES) - kWorkHead) / 4;
+    const int64_t spare = a.count < kCounted ? a.count + 1 : 0;  // tiles that are not full
+    const bool room = floats >= (uint64_t)(spare + 1) * tile_floats(p, 32);
+    // (of ranks above 128 h and its parts of 32 rows pass 64 KB of LDS)
+    const bool many = a.m > kGathered && (a.rank <= 128 || room);
     // rows that are gathered, or whose tiles there is room for, at once
     // (a dispatch counts its work-items in 32 bits)
     int64_t rows = std::min<int64_t>(a.m, many ? 1 << 20 : kGathered);
-    if (many && floats >= tile_floats(p, 32))
-        rows = std::min<int64_t>(rows, floats / tile_floats(p, 32) * 32);
+    if (many && room)
+        rows = std::min<int64_t>(rows, (floats / tile_floats(p, 32) - spare) * 32);
     for (int64_t i = 0; i < a.m; i += rows) {
         p.m = (int32_t)std::min(rows, a.m - i);
         p.x = static_cast<const T*>(a.x) + i * p.x_stride;

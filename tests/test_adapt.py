@@ -232,3 +232,47 @@ def test_refusals(work):
         assert torch.equal(held, t)
     refused("II_EOVERLAP", lambda: ops.ii_adapt(out, x, a, b, ids, base=torch.as_strided(out, (4, 32), (0, 1))))
     refused("II_EOVERLAP", lambda: ops.ii_adapt(room.view(BF16)[:128].view(4, 32), x, a, b, ids, work=room))
+
+
+@pytest.mark.parametrize("count", [900, 1023, 1024, 1500])
+@pytest.mark.parametrize("m", [300, 600, 2000])
+@pytest.mark.parametrize("run", [1, 40])
+def test_adapt_many_adapters(count, m, run, work):
+    """More adapters than rows, as many as are counted, and more."""
+    g = _gen(count + m)
+    x, base = _normal(g, m, 72), _normal(g, m, 40)
+    a, b = _normal(g, count, 8, 72, std=0.1), _normal(g, count, 40, 8, std=0.3)
+    ids = _ids(g, m, count, run)
+    out = torch.empty(m, 40, dtype=BF16, device=DEV)
+    for w in (work, None):
+        ops.ii_adapt(out, x, a, b, ids, base=base, work=w)
+        want, far = ref.adapt(x, a, b, ids, None, None, base)
+        _close(out, want, far)
+    assert not work[:65536].any()
+
+
+@pytest.mark.parametrize("rank", [16, 200])
+def test_adapt_order_is_replayed(rank, work):
+    """A captured call of many rows puts the adapters that it finds into order."""
+    g = _gen(rank)
+    m, n, k, count = 1700, 96, 160, 7
+    x, a, b = _normal(g, m, k), _normal(g, count, rank, k, std=0.1), _normal(g, count, n, rank, std=0.1)
+    ids, out = _ids(g, m, count), torch.empty(m, n, dtype=BF16, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ops.ii_adapt(out, x, a, b, ids, work=work, stream=side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        ops.ii_adapt(out, x, a, b, ids, work=work, stream=torch.cuda.current_stream())
+    for run in (1, 300, m):
+        ids.copy_(_ids(g, m, count, run))
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        _close(out, *ref.adapt(x, a, b, ids), f"runs of {run}")
+        again = torch.empty_like(out)
+        ops.ii_adapt(again, x, a, b, ids, work=work)     # whatever places the rows got
+        assert torch.equal(again, out)
