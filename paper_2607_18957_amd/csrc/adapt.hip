@@ -223,8 +223,7 @@ __global__ __launch_bounds__(kOrderThreads) void adapt_order(Adapt<T> p) {
     rows[t] = 0;
     __syncthreads();
     // takes a place for each lane's adapter (0: none), the lanes of one together
-    const auto take = [&](int* from, int64_t i) {
-        const int id = i < p.m ? adapter_of(p, i) + 1 : -1;
+    const auto take = [&](int* from, int id) {
         const int first = __builtin_amdgcn_readfirstlane(id);
         if (__ballot(id != first) == 0) {
             int at = 0;
@@ -233,7 +232,21 @@ __global__ __launch_bounds__(kOrderThreads) void adapt_order(Adapt<T> p) {
         }
         return id >= 0 ? atomicAdd(&from[id], 1) : 0;
     };
-    for (int64_t i = t; i - t < p.m; i += kOrderThreads) take(rows, i);
+    // put(row, adapter), some rows' adapters asked for at once
+    const auto each = [&](auto&& put) {
+        constexpr int kAhead = 4;
+        for (int64_t base = 0; base < p.m; base += kAhead * kOrderThreads) {
+            int id[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t i = base + u * kOrderThreads + t;
+                id[u] = i < p.m ? adapter_of(p, i) + 1 : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) put(base + u * kOrderThreads + t, id[u]);
+        }
+    };
+    each([&](int64_t, int id) { take(rows, id); });
     __syncthreads();
     static_assert(kCounted == kOrderThreads);
     const int held = t <= p.count ? rows[t] : 0, tiles = (held + kTok - 1) / kTok;
@@ -262,13 +275,13 @@ __global__ __launch_bounds__(kOrderThreads) void adapt_order(Adapt<T> p) {
         p.id[e] = -1;
     }
     __syncthreads();
-    for (int64_t i = t; i - t < p.m; i += kOrderThreads) {
-        const int e = take(next, i);
-        if (i < p.m) {
+    each([&](int64_t i, int id) {
+        const int e = take(next, id);
+        if (id >= 0) {
             p.row[e] = (int)i;
-            p.id[e] = adapter_of(p, i);
+            p.id[e] = id - 1;
         }
-    }
+    });
 }
 
 // The least adapter of the tile above a, or INT_MAX; its rank.
