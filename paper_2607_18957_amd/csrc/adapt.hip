@@ -16,7 +16,7 @@
 // one longer sum. f16 has little range: rows are brought to its middle by a power
 // of two first.
 //
-// A first kernel leaves the parts and the tiles' rows in `work`, a second one
+// A kernel leaves the parts and the tiles' rows in `work`, a second one
 // forms the columns of out, in waves that share nothing and never wait for one
 // another. Without `work`, and where the sums are short, each workgroup of a tile's
 // columns forms h again, in LDS.
