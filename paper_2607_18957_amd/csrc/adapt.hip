@@ -993,22 +993,21 @@ int check(const ii_adapt_args& a) {
         uint64_t rows, width;
         int64_t stride;
         uint64_t size;
-        bool need;
-    } ins[] = {{"x", a.x, m, k, a.x_stride, 2, true},
-               {"adapters", a.adapters, 1, m, 0, 4, true},
-               {"scales", a.scales, 1, (uint64_t)a.count, 0, 4, false},
-               {"ranks", a.ranks, 1, (uint64_t)a.count, 0, 4, false},
-               {"base", a.base, m, n, a.base_stride, bsize, false}};
+        bool need, in_place;
+    } ins[] = {{"x", a.x, m, k, a.x_stride, 2, true, false},
+               {"adapters", a.adapters, 1, m, 0, 4, true, false},
+               {"scales", a.scales, 1, (uint64_t)a.count, 0, 4, false, false},
+               {"ranks", a.ranks, 1, (uint64_t)a.count, 0, 4, false, false},
+               // each element of base is read by the lane that then writes it
+               {"base", a.base, m, n, a.base_stride, bsize, false,
+                a.base == a.out && osize == bsize && (m == 1 || a.base_stride == a.out_stride)}};
     for (const auto& in : ins) {
         if (!in.p && !in.need) continue;
         if (__builtin_mul_overflow((uint64_t)(in.rows > 1 ? in.stride : 0), in.size, &stride))
             return fail(II_EOVERFLOW, "%s: the stride of %s", fn, in.what);
         rc = check_rows(fn, in.what, in.p, in.rows, in.width * in.size, stride, in.size, &r);
         if (rc || (rc = check_apart(fn, in.what, scratch, r))) return rc;
-        // each element of base is read by the lane that then writes it
-        if (in.p == a.base && in.p == a.out && osize == bsize && (m == 1 || a.base_stride == a.out_stride))
-            continue;
-        if ((rc = check_apart(fn, in.what, out, r))) return rc;
+        if (!in.in_place && (rc = check_apart(fn, in.what, out, r))) return rc;
     }
     return II_OK;
 }
