@@ -127,6 +127,20 @@ int check_heads(const char* fn, const char* what, const void* p, int64_t tokens,
     return check_rows(fn, what, p, 1, span, 0, 16, r);
 }
 
+int check_heads_apart(const char* fn, const char* what, const Rows& written, const Nest& w,
+                      const Rows& read, const Nest& r) {
+    if (!written.rows || !read.rows) return II_OK;
+    // rows of what is read may meet each other, which nests_meet does not expect
+    uint64_t end = r.width;
+    bool apart = true;
+    for (int i = 0; i < r.axes; ++i) {
+        apart &= (uint64_t)r.by[i].stride >= end;
+        end += (uint64_t)(r.by[i].count - 1) * r.by[i].stride;
+    }
+    if (apart && !nests_meet(w, r)) return II_OK;
+    return check_apart(fn, what, written, read);
+}
+
 int check_cache(const char* fn, const ii_cache& c, bool written, CacheRows* held) {
     const bool quant = c.dtype == II_FP8_E4M3;
     if (!quant && !half_type(c.dtype)) return fail(II_EINVAL, "%s: cache of type %d", fn, c.dtype);
@@ -187,7 +201,7 @@ int check_move(const char* fn, const ii_cache& c, const ii_tokens& f, bool write
         return fail(II_EINVAL, "%s: %lld tokens", fn, (long long)f.tokens);
     if (!f.tokens) return II_OK;
     Rows &slots = r->slots, *rows = r->kv;
-    Nest nest[2];
+    Nest* nest = r->nest;
     rc = check_rows(fn, "slots", f.slots, 1, (uint64_t)f.tokens * 8, 0, 8, &slots);
     if (rc) return rc;
     const int64_t ts[2] = {f.k_token_stride, f.v_token_stride};

@@ -60,6 +60,10 @@ int check_heads(const char* fn, const char* what, const void* p, int64_t tokens,
                 int64_t dim, int64_t token_stride, int64_t head_stride, int size, bool written,
                 Rows* r, Nest* nest = nullptr);
 
+// check_apart for heads: those of one token may lie between another array's.
+int check_heads_apart(const char* fn, const char* what, const Rows& written, const Nest& w,
+                      const Rows& read, const Nest& r);
+
 // The memory of a cache: keys, values and their scales (empty without them).
 struct CacheRows {
     Rows all[4];
@@ -70,6 +74,7 @@ int check_cache(const char* fn, const ii_cache& c, bool written, CacheRows* held
 struct TokenRows {
     CacheRows cache;
     Rows kv[2], slots;  // slots and kv are empty without tokens
+    Nest nest[2];       // of kv, with tokens
 };
 int check_move(const char* fn, const ii_cache& c, const ii_tokens& f, bool write, TokenRows* r);
 

@@ -299,8 +299,8 @@ int check_rotary(const char* fn, const ii_rotary& r, int64_t tokens, int dim, Ro
     return rc;
 }
 
-// x and out of heads to be turned; out may be x itself.
-int check_turn(const char* fn, const ii_turn& t, Rows* x, Rows* out) {
+// x and out of heads to be turned; out may be x itself. *nest: out's, with tokens.
+int check_turn(const char* fn, const ii_turn& t, Rows* x, Rows* out, Nest* nest) {
     if (!half_type(t.dtype)) return fail(II_EINVAL, "%s: dtype %d", fn, t.dtype);
     if (t.heads < 1 || t.heads > 1 << 28) return fail(II_EINVAL, "%s: %d heads", fn, t.heads);
     if (t.dim < 8 || t.dim > 512 || t.dim % 8)
@@ -308,17 +308,18 @@ int check_turn(const char* fn, const ii_turn& t, Rows* x, Rows* out) {
     if (t.reserved) return fail(II_EINVAL, "%s: reserved is %d", fn, t.reserved);
     if (t.tokens < 0 || t.tokens > (int64_t)1 << 40)
         return fail(II_EINVAL, "%s: %lld tokens", fn, (long long)t.tokens);
+    Nest from;
     int rc = check_heads(fn, "x", t.x, t.tokens, t.heads, t.dim, t.x_token_stride, t.x_head_stride, 2,
-                         false, x);
+                         false, x, &from);
     if (!rc)
         rc = check_heads(fn, "out", t.out, t.tokens, t.heads, t.dim, t.out_token_stride,
-                         t.out_head_stride, 2, true, out);
+                         t.out_head_stride, 2, true, out, nest);
     if (rc) return rc;
     // a head is read by the lanes of a wave before any of them writes it
     if (t.x == t.out && (t.tokens <= 1 || t.x_token_stride == t.out_token_stride) &&
         (t.heads <= 1 || t.x_head_stride == t.out_head_stride))
         return II_OK;
-    return check_apart(fn, "x", *out, *x);
+    return check_heads_apart(fn, "x", *out, *nest, *x, from);
 }
 
 template <class T>
@@ -336,7 +337,8 @@ int rotate(const ii_turn* t, const ii_rotary* r, hipStream_t stream) {
     {
         const Checks checks;
         Rows x, out, held[2];
-        int rc = check_turn(fn, *t, &x, &out);
+        Nest nest;
+        int rc = check_turn(fn, *t, &x, &out, &nest);
         if (rc || (rc = check_rotary(fn, *r, t->tokens, t->dim, held))) return rc;
         if ((rc = check_apart(fn, "positions", out, held[0])) ||
             (rc = check_apart(fn, "freqs", out, held[1])))
@@ -377,6 +379,7 @@ int append(const ii_cache* c, const ii_tokens* f, const ii_rotary* r, const ii_t
         const Checks checks;
         TokenRows t;
         Rows x, out, held[2];
+        Nest nest;
         int rc = check_move(fn, *c, *f, true, &t);
         if (rc || (rc = check_rotary(fn, *r, f->tokens, c->dim, held))) return rc;
         if (c->heads > 1 << 28) return fail(II_EINVAL, "%s: cache of %d heads", fn, c->heads);
@@ -385,17 +388,22 @@ int append(const ii_cache* c, const ii_tokens* f, const ii_rotary* r, const ii_t
                 return fail(II_EINVAL, "%s: q of type %d, %lld tokens, %d elements; keys of type %d, "
                             "%lld, %d", fn, q->dtype, (long long)q->tokens, q->dim, f->dtype,
                             (long long)f->tokens, c->dim);
-            if ((rc = check_turn(fn, *q, &x, &out))) return rc;
+            if ((rc = check_turn(fn, *q, &x, &out, &nest))) return rc;
         }
         const struct {
             const char* what;
             const Rows& r;
-        } read[] = {{"k", t.kv[0]}, {"v", t.kv[1]}, {"slots", t.slots}, {"positions", held[0]},
-                    {"freqs", held[1]}, {"q", x}};
+            const Nest* nest;
+        } read[] = {{"k", t.kv[0], &t.nest[0]}, {"v", t.kv[1], &t.nest[1]}, {"slots", t.slots, nullptr},
+                    {"positions", held[0], nullptr}, {"freqs", held[1], nullptr}, {"q", x, nullptr}};
         for (const auto& in : read) {
             for (const Rows& w : t.cache.all)
                 if ((rc = check_apart(fn, in.what, w, in.r))) return rc;
-            if (&in.r != &x && (rc = check_apart(fn, in.what, out, in.r))) return rc;
+            if (&in.r == &x) continue;
+            // q may lie between the keys and values of its heads
+            rc = in.nest ? check_heads_apart(fn, in.what, out, nest, in.r, *in.nest)
+                         : check_apart(fn, in.what, out, in.r);
+            if (rc) return rc;
         }
         for (const Rows& w : t.cache.all)
             if ((rc = check_apart(fn, "the cache", out, w))) return rc;
