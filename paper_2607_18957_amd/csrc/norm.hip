@@ -153,12 +153,15 @@ __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void norm_rows(Nor
                 squares = fma(d, d, squares);
             }
         const double root = 1.0 / sqrt(row_sum<kThreads>(squares, turn++) / p.n + (double)p.eps);
-        const float r = (float)root, mu = (float)mean;
+        // The mean as two floats: rounded to one it is off by 2^-24 of itself, which
+        // is steps of the result where the deviation is that much smaller. y - mu is
+        // exact there, so what is left of the mean comes off after it, with the product.
+        const float r = (float)root, mu = (float)mean, rest = (float)(mean - mu) * r;
         if (r > 0x1p-100f && r < 0x1p100f) {
 #pragma unroll
             for (int w = 0; w < kWords; ++w)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[w][j] = (kLayer ? y[w][j] - mu : y[w][j]) * r;
+                for (int j = 0; j < 8; ++j) y[w][j] = kLayer ? fmaf(y[w][j] - mu, r, -rest) : y[w][j] * r;
         } else {  // what 32 bits cannot hold, of the root or of y - mean
 #pragma unroll
             for (int w = 0; w < kWords; ++w)
