@@ -44,7 +44,8 @@ struct Logprobs {
     float *logprob, *entropy, *top_logprobs;
     int64_t* top_ids;
     int64_t stride, rows;  // elements
-    int32_t vocab, top, parts, part;  // part: elements of one
+    int64_t part;          // elements of one, which may pass those of a vocabulary
+    int32_t vocab, top, parts;
     float scale;
     uint32_t* counters;
     float* partial;
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(kThreads, 3) void logprobs_rows(Logprobs p) {
         const T* logits = static_cast<const T*>(p.logits) + row * p.stride;
         const int lead = (int)(reinterpret_cast<uintptr_t>(logits) % 16 / sizeof(T));
         const vec* from = reinterpret_cast<const vec*>(logits - lead);
-        const int64_t begin = (int64_t)blockIdx.x * p.part;
+        const int64_t begin = blockIdx.x * p.part;
         const int64_t end = min(begin + p.part, (int64_t)p.vocab + lead);
         // asked for here, wanted at the end
         int64_t target = -1;
@@ -485,7 +486,7 @@ int run(const ii_logprobs_args& a, hipStream_t stream) {
         parts = std::max<int64_t>(parts, 1);
     }
     // a row may begin inside a word
-    p.part = (int32_t)(groups(groups(a.vocab + 7, parts), kThreads) * kThreads);
+    p.part = groups(groups(a.vocab + 7, parts), kThreads) * kThreads;
     p.parts = (int32_t)groups(a.vocab + 7, p.part);
     const dim3 grid(p.parts, (uint32_t)std::min<int64_t>(a.rows, 65535));
     if (a.top)
@@ -500,7 +501,7 @@ int check(const ii_logprobs_args& a) {
     if (!half_type(a.dtype) && a.dtype != II_F32) return fail(II_EINVAL, "%s: dtype %d", fn, a.dtype);
     if (a.top < 0 || a.top > II_MAX_TOP) return fail(II_EINVAL, "%s: top is %d", fn, a.top);
     if (a.reserved) return fail(II_EINVAL, "%s: reserved is %d", fn, a.reserved);
-    if (a.rows < 0 || a.rows > INT32_MAX || a.vocab < 1 || a.vocab > INT32_MAX - 16384)
+    if (a.rows < 0 || a.rows > INT32_MAX || a.vocab < 1 || a.vocab > INT32_MAX)
         return fail(II_EINVAL, "%s: %lld rows of %lld logits", fn, (long long)a.rows,
                     (long long)a.vocab);
     if (!std::isfinite(a.scale) || !(a.scale > 0)) return fail(II_EINVAL, "%s: scale %g", fn, a.scale);

@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 
 import fake_device  # noqa: E402
 from paper_2607_18957_amd import ii, ops  # noqa: E402
-from test_decoder_ops_abi import ADAPT, CACHE, ROTARY, TOKENS, TURN  # noqa: E402
+from test_decoder_ops_abi import ADAPT, CACHE, LOGPROBS, ROTARY, TOKENS, TURN  # noqa: E402
 
 AT = 1 << 40
 LET_THROUGH = "II_EHIP"     # nothing can be launched
@@ -122,3 +122,15 @@ def test_heads_that_meet_are_refused(call):
     for rc, m, a in zip(got, met, alike):
         assert rc in ("II_EOVERLAP", LET_THROUGH)
         assert rc == "II_EOVERLAP" if m else (rc == LET_THROUGH or not a)
+
+
+def _logprobs(**change):
+    return "ii_logprobs", [ops._LOGPROBS.pack(*{**LOGPROBS, **change}.values())]
+
+
+@pytest.mark.parametrize("dtype", [5, 6, 7])
+@pytest.mark.parametrize("work", [dict(), dict(work=1 << 50, work_bytes=64 << 20)])
+def test_logprobs_vocabularies(call, dtype, work):
+    """Up to 2^31 - 1 tokens, as the header says."""
+    for vocab, rc in (((1 << 31) - 1, LET_THROUGH), ((1 << 31) - 16384, LET_THROUGH), (1, LET_THROUGH), (1 << 31, "II_EINVAL")):
+        assert call(_logprobs(dtype=dtype, vocab=vocab, logits_stride=vocab, **work)) == [rc]
