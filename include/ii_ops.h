@@ -352,7 +352,7 @@ int ii_rotary_freqs(int32_t rot_dim, double base, double factor, double low, dou
  *   logprob, entropy, top_ids, top_logprobs   [rows] and [rows, top], packed;
  *            NULL: not wanted (logprob goes with targets, top_ids and
  *            top_logprobs with a top above 0).
- *   scale    positive and finite.
+ *   scale    positive, at most 2.3e38 (scale / ln 2 is a float).
  * Logits of -infinity have p = 0 and add nothing. In a row of nothing else every
  * log p is -infinity and the entropy 0. In a row that holds NaN or +infinity
  * log-probabilities and entropy are NaN; tokens are still in order, NaN above

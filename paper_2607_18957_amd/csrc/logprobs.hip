@@ -504,7 +504,9 @@ int check(const ii_logprobs_args& a) {
     if (a.rows < 0 || a.rows > INT32_MAX || a.vocab < 1 || a.vocab > INT32_MAX)
         return fail(II_EINVAL, "%s: %lld rows of %lld logits", fn, (long long)a.rows,
                     (long long)a.vocab);
-    if (!std::isfinite(a.scale) || !(a.scale > 0)) return fail(II_EINVAL, "%s: scale %g", fn, a.scale);
+    // exponentials are taken of scale / ln 2 times a difference, which may be 0
+    if (!std::isfinite(a.scale * kLog2e) || !(a.scale > 0))
+        return fail(II_EINVAL, "%s: scale %g", fn, a.scale);
     if (!a.rows) return II_OK;  // operands of no elements may be NULL
     if (!a.targets != !a.logprob)
         return fail(II_EINVAL, "%s: logprob and targets go together", fn);

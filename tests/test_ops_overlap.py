@@ -134,3 +134,10 @@ def test_logprobs_vocabularies(call, dtype, work):
     """Up to 2^31 - 1 tokens, as the header says."""
     for vocab, rc in (((1 << 31) - 1, LET_THROUGH), ((1 << 31) - 16384, LET_THROUGH), (1, LET_THROUGH), (1 << 31, "II_EINVAL")):
         assert call(_logprobs(dtype=dtype, vocab=vocab, logits_stride=vocab, **work)) == [rc]
+
+
+def test_logprobs_scales(call):
+    """A logit's exponential is taken of scale / ln 2 times it, a float."""
+    most = 2.3e38       # times 1.4427 the largest float
+    calls = [_logprobs(scale=s) for s in (most, 1e-38, 1e-45, 3.4028234e38, 2.4e38)]
+    assert call(*calls) == [LET_THROUGH] * 3 + ["II_EINVAL"] * 2
