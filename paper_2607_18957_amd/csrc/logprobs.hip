@@ -1,12 +1,13 @@
 // ii_logprobs: log-probabilities of given tokens, entropy and the likeliest
 // tokens, in one pass over the logits.
 //
-// Every thread keeps the running maximum m of its logits, s = sum e^(z - m) and
-// t = sum e^(z - m) (z - m); then log sum_j e^z_j = m + log s, and the entropy is
-// log s - t / s. Sums of a tile are added up in 64 bits: a vocabulary is a long
-// sum, and what it loses is in every result. A logit is kept as a key of 64 bits,
-// its order above and its token's complement below, so that no two are alike and
-// the order of arrival does not show.
+// Every thread keeps the running maximum m of its logits, s = sum 2^u and t = sum
+// 2^u u, u = (z - m) / ln 2, a term of which is never below -0.54 however far apart
+// the logits are; then log sum_j e^z_j = m + log s, and the entropy is log s - t ln 2
+// / s. Sums of a tile are added up in 64 bits: a vocabulary is a long sum, and what
+// it loses is in every result. A logit is kept as a key of 64 bits, its order above
+// and its token's complement below, so that no two are alike and the order of
+// arrival does not show.
 //
 // The likeliest tokens: of the largest logits of a wave's 64 threads, in order, the
 // top-th is a bound that `top` tokens reach, and so is the least of the waves'
@@ -52,7 +53,7 @@ struct Logprobs {
     uint32_t room;  // floats of a part in partial
 };
 
-// Sums of e^(z - m), and of (x - m) times that, x a logit. `to2` is scale / ln 2.
+// Sums of 2^u, and of u times that, u = (x - m) to2, x a logit; to2 is scale / ln 2.
 struct Sums {
     float m;
     double s, t;
@@ -68,9 +69,9 @@ __device__ inline void move_to(Sums& a, float m, float to2) {
         if (a.m == -INFINITY) {
             a.t = 0;
         } else {
-            const float d = a.m - m;
-            const double c = exp2_of(d * to2);
-            a.t = c * (a.t + a.s * fmaxf(d, -3e38f));
+            const float u = (a.m - m) * to2;
+            const double c = exp2_of(u);
+            a.t = c * (a.t + a.s * fmaxf(u, -3e38f));
             a.s *= c;
         }
         a.m = m;
@@ -232,6 +233,7 @@ __global__ __launch_bounds__(kThreads, 3) void logprobs_rows(Logprobs p) {
     List& list = *reinterpret_cast<List*>(lds);
     const int t = threadIdx.x;
     const float to2 = p.scale * kLog2e;
+    const double unit = p.scale / (double)to2;  // of u in z
 
     for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
         // Words are whole ones of memory: tokens before the row's first and past
@@ -286,9 +288,9 @@ __global__ __launch_bounds__(kThreads, 3) void logprobs_rows(Logprobs p) {
             float s = 0, below = 0;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const float d = x[i] - ref, e = exp2_of(d * to2);
+                const float u = (x[i] - ref) * to2, e = exp2_of(u);
                 s += e;
-                below = fmaf(e, fmaxf(d, -3e38f), below);
+                below = fmaf(e, fmaxf(u, -3e38f), below);
             }
             sums.s += s;
             sums.t += below;
@@ -427,10 +429,9 @@ __global__ __launch_bounds__(kThreads, 3) void logprobs_rows(Logprobs p) {
         const bool none = sums.m == -INFINITY && sums.s == 0;
         // The exponentials were of z (1 + off), as scale / ln 2 was rounded: their
         // sum's logarithm is off by off times the mean of z - m, the same way in
-        // every term, where other roundings cancel.
-        const double mean = none ? 0.0 : p.scale * (sums.t / sums.s);
-        const double off = (double)to2 / (p.scale * 1.4426950408889634) - 1;
-        const double logs = none ? 0.0 : log(sums.s) - off * mean;
+        // every term, where other roundings cancel. unit / ln 2 is 1 - off.
+        const double mean = none ? 0.0 : unit * (sums.t / sums.s);
+        const double logs = none ? 0.0 : log(sums.s) + fma(mean * unit, 1.4426950408889634, -mean);
         const auto result = [&](float x) {
             return none ? -INFINITY : (float)(((double)x - sums.m) * p.scale - logs);
         };

@@ -12,6 +12,8 @@ if not torch.cuda.is_available():  # collected on CPU machines, never run there
 
 from paper_2607_18957_amd import ops  # noqa: E402  (fails loudly if libii.so is missing)
 
+import decoder_ref as ref  # noqa: E402
+
 DEV = torch.device("cuda:0")
 BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
 E = 2.0 ** -24
@@ -41,3 +43,25 @@ def test_largest_vocabulary(dt, vocab, split):
     for got, want in [(logprob[0].item(), 12 - log), *zip(tops[0].tolist(), (13 - log, 12 - log, 12 - log, -log, -log))]:
         assert abs(got - want) <= off + abs(want) * E
     assert abs(entropy.item() - (log - mean)) <= off * (2 + 2 * 13) + (log - mean) * E
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 8192), (3, 20001)])
+@pytest.mark.parametrize("scale", [1e-38, 3e-39, 1e-40])
+@pytest.mark.parametrize("split", [False, True])
+def test_logits_far_apart(rows, vocab, scale, split):
+    """Logits of 1e38 to either side, scaled to a few units: what is summed is within
+    range only once it is scaled. 2 E (40 + 2 mean) as for other logits."""
+    g = torch.Generator(device=DEV).manual_seed(vocab)
+    x = (torch.rand(rows, vocab, generator=g, device=DEV) * 2 - 1) * 1.6e38
+    x[-1, ::2], x[-1, 1::2] = 1.6e38, -1.6e38
+    targets = torch.arange(rows, device=DEV) + vocab // 2
+    logprob, entropy = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    ids, tops = torch.empty(rows, 5, dtype=torch.int64, device=DEV), torch.empty(rows, 5, device=DEV)
+    ops.ii_logprobs(x, targets=targets, logprob=logprob, entropy=entropy, top_ids=ids, top_logprobs=tops, scale=scale,
+                    work=ops.work_buffer() if split else None)
+    logp, off, h, far = ref.logprobs(x, scale)
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :5]
+    assert torch.equal(ids, order)
+    for got, want, bound in ((logprob, logp.gather(1, targets[:, None])[:, 0], off.gather(1, targets[:, None])[:, 0]),
+                             (entropy, h, far), (tops, logp.gather(1, order), off.gather(1, order))):
+        assert bool(((got.double() - want).abs() <= bound).all()), (got, want)
