@@ -166,7 +166,7 @@ class Cache:
 
 
 def _tokens(cache: Cache, k, v, slots) -> bytes:
-    t, dt = k.shape[0], k.dtype
+    (t, _, _), dt = k.shape, k.dtype
     _fits(k.shape == v.shape == (t, cache.heads, cache.dim) and v.dtype == dt,
           "k and v are not [tokens, heads, dim] of one type")
     _fits(slots.shape == (t,) and slots.dtype == torch.int64 and (t < 2 or slots.stride(0) == 1),
@@ -301,12 +301,14 @@ def ii_cache_append(cache: Cache, k, v, slots, positions, freqs, *, q=None, q_ou
     may be q."""
     _fits((q is None) == (q_out is None), "q and q_out go together")
     turn = None
+    tokens, _, _ = k.shape
     if q is not None:
-        _fits(q.shape[0] == k.shape[0] and q.shape[2] == cache.dim and q.dtype == k.dtype,
+        rows, _, dim = q.shape
+        _fits(rows == tokens and dim == cache.dim and q.dtype == k.dtype,
               "q is not [tokens, heads, dim] of the keys' type")
         turn = _turn(q_out, q)
     rc = _call_append(cache.args, _tokens(cache, k, v, slots),
-                      _rotary(k.shape[0], positions, freqs, layout, magnitude), turn, ii._stream(stream))
+                      _rotary(tokens, positions, freqs, layout, magnitude), turn, ii._stream(stream))
     if rc:
         ii._check(rc, "ii_cache_append")
 
@@ -325,7 +327,7 @@ def ii_logprobs(logits, *, targets=None, logprob=None, entropy=None, top_ids=Non
     _fits((targets is None) == (logprob is None), "targets and logprob go together")
     ids = values = 0
     if top_ids is not None:
-        top = top_ids.shape[1]
+        _, top = top_ids.shape
         _fits(top_ids.shape == top_logprobs.shape == (rows, top) and top_ids.is_contiguous()
               and top_logprobs.is_contiguous() and top_ids.dtype == i64 and top_logprobs.dtype == f32,
               "top_ids and top_logprobs are not contiguous [rows, top] of int64 and float32")
@@ -346,7 +348,7 @@ def ii_adapt(out, x, a, b, adapters, *, scales=None, ranks=None, base=None, work
     rank, k], b [count, n, rank], of which adapter c uses the first ranks[c] rows
     and columns. base [m, n] may be out; either may be float32."""
     (m, k), (count, rank, ka), dt = x.shape, a.shape, x.dtype
-    n = b.shape[1]
+    _, n, _ = b.shape
     _fits(ka == k and b.shape == (count, n, rank) and a.dtype == b.dtype == dt and out.shape == (m, n),
           "shapes or types of out, x, a, b differ")
     ac, ar, al = a.stride()
