@@ -355,8 +355,9 @@ int ii_rotary_freqs(int32_t rot_dim, double base, double factor, double low, dou
  *   scale    positive, at most 2.3e38 (scale / ln 2 is a float).
  * Logits of -infinity have p = 0 and add nothing. In a row of nothing else every
  * log p is -infinity and the entropy 0. In a row that holds NaN or +infinity
- * log-probabilities and entropy are NaN; tokens are still in order, NaN above
- * all (magnitudes of scale * logits past 32 bits count as infinite).
+ * log-probabilities and entropy are NaN; tokens are still in order, those of NaN
+ * as if they were -infinity (magnitudes of scale * logits past 32 bits count as
+ * infinite).
  * Errors: II_EINVAL, II_EALIGN, II_EOVERFLOW, II_EOVERLAP, II_EHIP.
  */
 #define II_MAX_TOP 64

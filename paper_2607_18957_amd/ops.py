@@ -317,8 +317,8 @@ def ii_logprobs(logits, *, targets=None, logprob=None, entropy=None, top_ids=Non
                 scale: float = 1.0, work=None, stream=None) -> None:
     """From logits [rows, vocab], times scale: log-probabilities of targets [rows]
     into logprob [rows], the entropy of each row into entropy [rows], the largest
-    logits' tokens, equal ones in their order, into top_ids [rows, top] and their
-    log-probabilities into top_logprobs."""
+    logits' tokens, equal ones in their order and NaN as -infinity, into top_ids
+    [rows, top] and their log-probabilities into top_logprobs."""
     rows, vocab = logits.shape
     at, stride = _rows(logits, "logits")
     f32, i64 = torch.float32, torch.int64
