@@ -19,8 +19,8 @@
  *     that may overlap on different streams need scratch of their own. NULL
  *     (0 bytes) means that nothing is split, which is slower for few rows.
  *     II_WORK_BYTES is as much as any call makes use of; that much of it may
- *     not meet what else the call reads or writes (II_EOVERLAP). The same inputs,
- *     strides and work_bytes give the same bits.
+ *     not meet what else the call reads or writes (II_EOVERLAP). The same inputs
+ *     at the same strides, work_bytes and addresses modulo 16 give the same bits.
  */
 #ifndef II_OPS_H
 #define II_OPS_H
@@ -215,7 +215,7 @@ enum {
  *   sum[i] = scale * gate[i] * y[i] + residual[i]
  *   out[i] = N(sum[i]; weight, bias)
  *
- * All of it is held in 32 bits, the norms' sums in 64; sum and out are each
+ * All of it is held in 32 bits, the norms' sums and means in 64; sum and out are each
  * rounded once (out is of sum as it was before).
  *
  *   dtype         of x, gate, weights, biases and out: II_BF16 or II_F16.
@@ -273,7 +273,7 @@ enum {
  * far positions keep their angle, products in 32, those of keys that are
  * quantised in 64; each result is rounded once.
  *
- *   positions  of each token; any whose angles are below 2^50 radians.
+ *   positions  of each token, of magnitudes up to 2^53 and angles below 2^50 radians.
  *   freqs      rot_dim / 2 frequencies in radians a position (ii_rotary_freqs).
  *   rot_dim    even, 0 to the heads' dim.
  *   magnitude  finite.
@@ -342,7 +342,8 @@ int ii_rotary_freqs(int32_t rot_dim, double base, double factor, double low, dou
  *   top_ids    the `top` tokens of the largest logits, largest first, equal ones
  *              by their number; top_logprobs their log p
  *
- * Exponentials are held in 32 bits, their sums in 64; each result is rounded once.
+ * Exponentials and sums of 32 of them are held in 32 bits, longer sums in 64; each
+ * result is rounded once.
  *
  *   dtype    of the logits: II_F32, II_BF16 or II_F16.
  *   rows     0 to 2^31 - 1.
@@ -356,8 +357,9 @@ int ii_rotary_freqs(int32_t rot_dim, double base, double factor, double low, dou
  * Logits of -infinity have p = 0 and add nothing. In a row of nothing else every
  * log p is -infinity and the entropy 0. In a row that holds NaN or +infinity
  * log-probabilities and entropy are NaN; tokens are still in order, those of NaN
- * as if they were -infinity (magnitudes of scale * logits past 32 bits count as
- * infinite).
+ * as if they were -infinity. Logits that differ from their row's largest by more
+ * than 32 bits hold (3.4e38) add nothing, and log-probabilities below what they hold
+ * are -infinity.
  * Errors: II_EINVAL, II_EALIGN, II_EOVERFLOW, II_EOVERLAP, II_EHIP.
  */
 #define II_MAX_TOP 64
@@ -386,7 +388,8 @@ int ii_logprobs(const ii_logprobs_args* args, hipStream_t stream);
  *
  * Rows whose adapter is negative or not below `count` get base alone. Products
  * are summed in 32 bits, h goes into the second product with 16 bits or more
- * (24 where out is II_F32); out is rounded once.
+ * (24 where out is II_F32), in parts that are multiplied apart: where an element of
+ * b is infinite, NaN may take the place of an infinite result. out is rounded once.
  *
  *   dtype       of x, a, b: II_BF16 or II_F16; base_dtype and out_dtype: dtype or
  *               II_F32.
