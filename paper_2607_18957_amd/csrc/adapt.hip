@@ -22,7 +22,7 @@
 // columns forms h again, in LDS.
 //
 // Many rows are bound by memory: 4099 x 4096 x 14336 with 8 adapters of rank 64 and
-// a base of 32 bits 121 us, the second kernel 90 of them at 3.9 TB/s. Few are bound
+// a base of 32 bits 121 us, the second kernel 89 of them at 4.0 TB/s. Few are bound
 // by the steps from one kernel's first load to the other's last store: 250 x 14336 x
 // 4096 with 32 adapters of rank 16 20 us, 4 x 4096 x 4096 12, a call's cost on the
 // host being 10.
@@ -833,6 +833,11 @@ void share_columns(Adapt<T>& p, int columns, int64_t tiles, int64_t wanted) {
 template <class T, int kTok, int kTT, int kC>
 void expand_launch(Adapt<T> p, int64_t tiles, hipStream_t stream) {
     share_columns(p, 4 / (kTok / (kTT * 16)) * kC * 16, tiles, 4096);
+    // Parts of h in registers, or read again for every 64 columns. 250 x 14336 x 4096
+    // with 32 adapters takes 18.3 us with rank 8, 18.5 with 16, 22.4 (24), 22.7 (32),
+    // 28.4 (48), 31.8 (64), 63.0 (128); 4099 x 4096 x 14336 with 8 adapters 87, 86,
+    // 98, 88, 112, 108, 226; with a result of 32 bits, three parts, 118 with rank 16
+    // and 196 with 64. Rank 128 would take 64 registers a lane for its parts alone.
     const int fast = p.parts == 2 ? p.rankp : 0;
     if (fast == 16) return expand_base<T, kTok, kTT, kC, 16>(p, stream);
     if (fast == 32) return expand_base<T, kTok, kTT, kC, 32>(p, stream);

@@ -18,10 +18,12 @@
 // that reach it. A list is cut to `top` by counting, for each key, those above it,
 // after a bound of the same kind has left few.
 //
-// Bound by memory: 2047 x 128256 in bf16 100 us, 5.2 TB/s, where a logit takes some
-// ten vector instructions, of which the exponential counts for four. Few rows are
-// bound by the steps from a load to the last part's joining: 48 x 128256 with the 20
-// likeliest 22 us, 1 x 8192 with 5 of them 8.6.
+// Bound by memory: 2047 x 128256 in bf16 101 us, 5.2 TB/s, where a logit takes some
+// ten vector instructions, of which the exponential counts for four; in the first
+// milliseconds of load the card takes up to 130. With the 5 or 20 likeliest, 240 and
+// 257 us, the vector units bound it. Few rows are bound by the steps from a load to
+// the last part's joining: 48 x 128256 with the 20 likeliest 22 us, 1 x 8192 with 5
+// of them 8.8.
 #include <algorithm>
 #include <cmath>
 
@@ -223,6 +225,8 @@ struct Word {  // 16 bytes of logits
     static constexpr int size = 16 / sizeof(T);
 };
 
+// Three workgroups a compute unit leave a lane 168 registers; of f32 with the
+// likeliest one more is kept in scratch, read once a row.
 template <class T, bool kTop>
 __global__ __launch_bounds__(kThreads, 3) void logprobs_rows(Logprobs p) {
     constexpr int kWord = Word<T>::size, kWords = kEach / kWord;

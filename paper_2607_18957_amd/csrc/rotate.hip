@@ -15,7 +15,7 @@
 //
 // Bound by memory: 8191 tokens of 32 heads of 128, turned in half of each, 29.7 us,
 // 4.5 TB/s; 16384 tokens appended to an 8-bit cache, 32 query and 8 key heads,
-// 95 us, 3.9 TB/s. The loads of four rounds are on their way, 4 KB a wave: with one
+// 92 us, 4.0 TB/s. The loads of four rounds are on their way, 4 KB a wave: with one
 // these took 36 and 117 us, with eight, which leave fewer waves, 29 and 103.
 #include <algorithm>
 #include <cmath>
